@@ -301,6 +301,133 @@ seka_status seka_learn_projection(const void* h_neutral, const void* h_signal, c
 seka_status seka_head_distance(const void* h_pos, const void* h_neg, const seka_shape* sh, float* D_out,
                                void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/*
+ * Caches of pages (continuous batching: chunks of prompts and generation steps of many requests in one call).
+ *
+ * Keys and values of all requests live in one pool of pages; token j of request b lies in page table[b, j / page_size] at
+ * slot j % page_size.  Keys are stored as they are attended to: edited (seka_edit_keys_packed on a chunk's keys before they
+ * are appended) and turned to their positions.  What a call covers: new tokens are packed rows, request b owns rows
+ * cu_seqlens[b] .. cu_seqlens[b+1]-1, the first max_q of them; they are the LAST n tokens of its cache, so new token i is
+ * cached token lens[b] - n + i (lens counts the tokens with the new ones, before and after the chunk's keys are written).
+ * Every length, offset and page number is clamped on the device, so no content of cu_seqlens, lens or table can make a
+ * kernel leave the tensors; rows that belong to no request are left untouched.
+ */
+typedef struct {
+  void* K;                /* dev [num_pages, page_size, Hkv, D] tensor dtype                        */
+  void* V;                /* dev, like K                                                            */
+  float* W;               /* dev [num_pages, Hkv, page_size] fp32: attention that each cached token got
+                             (seka_attention_weights), or NULL where a call does not need it        */
+  const int32_t* table;   /* dev [B, max_pages] page numbers                                        */
+  const int32_t* lens;    /* dev [B] cached tokens per request                                      */
+  int32_t num_pages;
+  int32_t page_size;      /* a power of two, 8 .. 65536                                             */
+  int32_t max_pages;      /* row length of the table                                                */
+} seka_paged;
+
+/* Rotary positions: pair i of a head's first `dim` elements turns by position * freq[i] radians, the rest is copied. */
+typedef struct {
+  int32_t dim;            /* even, 2 .. D                                                           */
+  int32_t interleaved;    /* 0: pair i is elements (i, i + dim/2); else (2i, 2i + 1)                */
+  const double* freq;     /* host [dim/2] radians per position (seka_rope_frequencies, or any finite values) */
+  float factor;           /* of cosine and sine (attention temperature of stretched contexts); 0 means 1 */
+} seka_rope;
+
+typedef enum {
+  SEKA_ROPE_PLAIN = 0,    /* f_i = base^(-2i/dim)                                                   */
+  SEKA_ROPE_LINEAR = 1,   /* f_i / stretch                                                          */
+  SEKA_ROPE_BASE = 2,     /* base raised to base * stretch^(dim/(dim-2)): the slowest pair is stretched, the fastest kept */
+  SEKA_ROPE_PARTS = 3,    /* by the turns t_i = original f_i / 2pi that a pair makes over the original context: kept above `fast`
+                             turns, f_i / stretch below `slow`, between them mixed linearly in the pair's index, from
+                             floor(i(fast)) to ceil(i(slow)), i(t) = dim ln(original / (2pi t)) / (2 ln base)         */
+  SEKA_ROPE_TURNS = 4     /* the same ends, between them mixed linearly in t_i                      */
+} seka_rope_scaling;
+
+/*
+ * seka_rope_frequencies — radians per position of the dim/2 pairs (host only, no GPU).  base > 1; stretch >= 1 (context
+ * length over the original one; ignored by PLAIN); original, fast, slow (fast > slow > 0) matter to PARTS and TURNS only.
+ */
+seka_status seka_rope_frequencies(int32_t dim, double base, int32_t scaling, double stretch, double original, double fast,
+                                  double slow, double* freq_out);
+
+/*
+ * seka_rotary — queries and keys turned to their positions, between projection or key edit and attention.
+ *   out = factor * (x cos - y sin, y cos + x sin) for each pair (x, y), angles formed in 64 bits, one rounding to the dtype
+ *
+ * Q, Q_out  dev [B,S,Hq,D];  K, K_out dev [B,S,Hkv,D] or both NULL;  tensor dtype.  Q_out == Q and K_out == K are allowed,
+ *           any other overlap is SEKA_ERR_ALIAS.  (A packed batch is B = 1, S = total_tokens, with positions.)
+ * positions dev [B*S] int32, any values, or NULL: token t of every row of the batch has position t.
+ * The inverse rotation is the one of -freq.
+ */
+seka_status seka_rotary(const void* Q, void* Q_out, const void* K, void* K_out, const seka_shape* sh, const seka_rope* rope,
+                        const int32_t* positions, void* hip_stream);
+
+/*
+ * seka_cache_append — a chunk's keys (turned, if rope is given) and values into the pages, its queries turned beside them.
+ *
+ * K, V       dev [total_tokens,Hkv,D] tensor dtype.
+ * Q, Q_out   dev [total_tokens,Hq,D] or both NULL; Q_out == Q is allowed.  Without rope they have to be NULL.
+ * positions  dev [total_tokens] int32, or NULL: a token's position is its index in the cache (a cache that was cut by
+ *            seka_cache_evict holds tokens whose positions run ahead of it).
+ * mask       dev [total_tokens] or NULL: with cache->W, the new tokens' weights start at 0, those of highlighted ones (nonzero)
+ *            at +infinity, which no eviction prefers another to.
+ * sh->S      the most cached tokens of a request; tokens that lie beyond it, or beyond the table, are not written.
+ * No two requests' new tokens may share a page slot.
+ */
+seka_status seka_cache_append(const void* K, const void* V, const void* Q, void* Q_out, const seka_shape* sh,
+                              const seka_paged* cache, const seka_rope* rope, const int32_t* positions, const uint8_t* mask,
+                              const int32_t* cu_seqlens, int64_t total_tokens, int32_t max_q, void* hip_stream);
+
+/*
+ * seka_attention_chunk — new tokens attend to their request's cache of pages, their own keys included: single tokens
+ * (generation), chunks of prompts and whole prompts, mixed in a batch.  New token i sees cached tokens 0 .. lens[b] - n + i.
+ *
+ * Q, O       dev [total_tokens,Hq,D] tensor dtype.
+ * lse        dev [Hq,total_tokens] fp32 or NULL: natural log of the softmax denominator.
+ * sh->S      the most cached tokens of a request (it sizes the launch; longer caches are cut to their first S tokens).
+ * max_q      the longest chunk, 1 .. S.
+ * A token that sees no key (lens[b] smaller than n) gets O = 0 and lse = -inf.  Keys and values behind lens[b] are never read.
+ * workspace  dev scratch of at least seka_chunk_workspace_bytes(...) bytes, 16-byte aligned; contents on return are
+ *            unspecified; calls sharing it must be ordered by their stream.
+ * Deterministic for given arguments and lengths.  A token's bits may differ with the batch it is in (its keys are then cut into
+ * other ranges), within rounding.
+ */
+size_t seka_chunk_workspace_bytes(const seka_shape* sh, int64_t total_tokens, int32_t max_q);
+seka_status seka_attention_chunk(const void* Q, void* O, float* lse, const seka_shape* sh, const seka_paged* cache,
+                                 const int32_t* cu_seqlens, int64_t total_tokens, int32_t max_q, void* workspace,
+                                 size_t workspace_bytes, void* hip_stream);
+
+/*
+ * seka_attention_weights — the attention that every cached token gets, summed over a chunk's queries and the heads of its group:
+ *   W[b,h,j] = decay * W_in[b,h,j] + sum_g sum_i exp(scale q_{i,g} . k_j - lse_{i,g}),  the last `window` new tokens i that see j
+ * for all cached tokens j < lens[b]; other slots are left untouched.
+ *
+ * Q          dev [total_tokens,Hq,D] as given to seka_attention_chunk;  lse dev [Hq,total_tokens], its result.
+ * cache->W   dev (written; required);  W_in dev, same layout, may be cache->W itself, or NULL: the sums alone.
+ * window     >= 1; max_q and more: all new tokens.  decay: finite; 0 does not read W_in.
+ * Tokens with lse = -inf count nothing.  Deterministic.
+ */
+seka_status seka_attention_weights(const void* Q, const float* lse, const seka_shape* sh, const seka_paged* cache,
+                                   const float* W_in, const int32_t* cu_seqlens, int64_t total_tokens, int32_t max_q,
+                                   int32_t window, float decay, void* hip_stream);
+
+/*
+ * seka_cache_evict — cuts every request's cache to `budget` tokens per KV head: the last `recent` ones and, of the others, the
+ * budget - recent with the largest weights src->W (equal ones: the earlier token; NaN below everything).  Heads keep tokens of
+ * their own; the kept ones keep their order and move to slots 0 .. of dst with their keys, values and weights, bit for bit.  A
+ * request of no more than `budget` tokens keeps them all.
+ *
+ * src, dst   pools; src->W and dst->W required.  dst->table == src->table with the same K, V, W, num_pages and page_size cuts in place.
+ *            Otherwise the pages that dst's table names for the kept tokens must not be pages that src's tables name for cached
+ *            ones.  dst may be pages of the same pool or another one; no part of one tensor may overlap a different one.
+ *            dst->lens is not read.  dst->table has to hold min(budget, S) tokens.  No page may belong to two requests.
+ * kept       dev [B,Hkv,budget] int32 (written): the kept tokens' former indices, ascending; -1 behind a shorter cache.
+ * lens_out   dev [B] int32 (written): min(lens[b], budget).  Not src->lens.
+ * sh->S      the most cached tokens of a request (longer ones are cut to their first S first);  sh->Hq is ignored.
+ * 1 <= budget, 0 <= recent <= budget.
+ */
+seka_status seka_cache_evict(const seka_shape* sh, const seka_paged* src, const seka_paged* dst, int32_t budget, int32_t recent,
+                             int32_t* kept, int32_t* lens_out, void* hip_stream);
+
 /* Name of a status code; static storage, never NULL. */
 const char* seka_status_string(int32_t status);
 

@@ -24,6 +24,7 @@ lib = ctypes.CDLL(LIB_PATH)
 SEKA_OK = 0
 SEKA_F32, SEKA_BF16 = 0, 1
 SEKA_ROUTE_SOFTMAX_COS, SEKA_ROUTE_PAPER_EQ6 = 0, 1
+SEKA_ROPE_PLAIN, SEKA_ROPE_LINEAR, SEKA_ROPE_BASE, SEKA_ROPE_PARTS, SEKA_ROPE_TURNS = range(5)
 SEKA_MAX_RANK, SEKA_MAX_KV_HEADS, SEKA_MAX_EXPERTS = 128, 64, 16
 
 
@@ -36,6 +37,17 @@ class seka_steer(ctypes.Structure):
     _fields_ = [("M", ctypes.c_int32), ("r", ctypes.c_int32), ("U", ctypes.c_void_p), ("w", ctypes.c_void_p),
                 ("gain", ctypes.POINTER(ctypes.c_float)), ("mask", ctypes.c_void_p),
                 ("key_scale", ctypes.POINTER(ctypes.c_float))]
+
+
+class seka_paged(ctypes.Structure):
+    _fields_ = [("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("W", ctypes.c_void_p), ("table", ctypes.c_void_p),
+                ("lens", ctypes.c_void_p), ("num_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32)]
+
+
+class seka_rope(ctypes.Structure):
+    _fields_ = [("dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("freq", ctypes.POINTER(ctypes.c_double)),
+                ("factor", ctypes.c_float)]
 
 
 _vp, _i32, _f32, _sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_float, ctypes.c_size_t
@@ -81,6 +93,22 @@ lib.seka_attention_prefill_packed.restype = _i32
 lib.seka_attention_prefill_packed.argtypes = [_vp, _vp, _vp, _vp, _vp, _shape_p, _steer_p, _vp, ctypes.c_int64, _vp]
 lib.seka_attention_plain.restype = _i32
 lib.seka_attention_plain.argtypes = [_vp, _vp, _vp, _vp, _vp, _shape_p, _vp]
+
+_paged_p, _rope_p, _i64, _f64 = ctypes.POINTER(seka_paged), ctypes.POINTER(seka_rope), ctypes.c_int64, ctypes.c_double
+lib.seka_rope_frequencies.restype = _i32
+lib.seka_rope_frequencies.argtypes = [_i32, _f64, _i32, _f64, _f64, _f64, _f64, ctypes.POINTER(_f64)]
+lib.seka_rotary.restype = _i32
+lib.seka_rotary.argtypes = [_vp, _vp, _vp, _vp, _shape_p, _rope_p, _vp, _vp]
+lib.seka_cache_append.restype = _i32
+lib.seka_cache_append.argtypes = [_vp, _vp, _vp, _vp, _shape_p, _paged_p, _rope_p, _vp, _vp, _vp, _i64, _i32, _vp]
+lib.seka_chunk_workspace_bytes.restype = _sz
+lib.seka_chunk_workspace_bytes.argtypes = [_shape_p, _i64, _i32]
+lib.seka_attention_chunk.restype = _i32
+lib.seka_attention_chunk.argtypes = [_vp, _vp, _vp, _shape_p, _paged_p, _vp, _i64, _i32, _vp, _sz, _vp]
+lib.seka_attention_weights.restype = _i32
+lib.seka_attention_weights.argtypes = [_vp, _vp, _shape_p, _paged_p, _vp, _vp, _i64, _i32, _i32, _f32, _vp]
+lib.seka_cache_evict.restype = _i32
+lib.seka_cache_evict.argtypes = [_shape_p, _paged_p, _paged_p, _i32, _i32, _vp, _vp, _vp]
 
 
 class SekaError(RuntimeError):
@@ -357,3 +385,158 @@ def seka_attention_prefill_packed(Q, K, V, O, cu_seqlens, max_len, U=None, gain=
                                              ctypes.byref(sh), st, _dev(cu_seqlens, "cu_seqlens"), total,
                                              _stream(stream)))
     return O
+
+
+# ---- caches of pages ----------------------------------------------------------------------------------------------------
+
+
+class Rope:
+    """Rotation of a head's first 2 len(freq) elements; made once, handed to every call."""
+
+    def __init__(self, freq, interleaved=False, factor=1.0):
+        n = len(freq)
+        self.freq = (ctypes.c_double * n)(*[float(f) for f in freq])
+        self.struct = seka_rope(2 * n, 1 if interleaved else 0, self.freq, float(factor))
+        self.ref = ctypes.byref(self.struct)
+
+
+def rope(freq, interleaved=False, factor=1.0):
+    """freq: radians per position of every pair (seka_rope_frequencies); interleaved: pairs (2i, 2i + 1) instead of (i, i + n)."""
+    return Rope(freq, interleaved, factor)
+
+
+def seka_rope_frequencies(dim, base=10000.0, scaling=SEKA_ROPE_PLAIN, stretch=1.0, original=0.0, fast=32.0, slow=1.0):
+    """Radians per position of the dim / 2 pairs, as a list of floats."""
+    out = (ctypes.c_double * max(dim // 2, 1))()
+    _check(lib.seka_rope_frequencies(dim, float(base), scaling, float(stretch), float(original), float(fast), float(slow), out))
+    return list(out)
+
+
+class PagedCache:
+    """One pool of pages with the page table and lengths of a batch; made once, handed to every call.  lens and table are device
+    tensors that the program may update in place between calls."""
+
+    def __init__(self, K, V, table, lens, W=None):
+        if K.dim() != 4 or V.shape != K.shape or V.dtype != K.dtype:
+            raise ValueError("K and V must be [num_pages, page_size, Hkv, D] of one dtype")
+        if table.dim() != 2 or table.dtype != torch.int32 or lens.dtype != torch.int32 or lens.numel() != table.shape[0]:
+            raise ValueError("table must be int32 [B, max_pages], lens int32 [B]")
+        pages, self.page_size, self.Hkv, self.D = K.shape
+        if W is not None and (W.dtype != torch.float32 or tuple(W.shape) != (pages, self.Hkv, self.page_size)):
+            raise ValueError(f"W must be fp32 [num_pages={pages}, Hkv={self.Hkv}, page_size={self.page_size}]")
+        if any(t.device != K.device for t in (V, table, lens)) or (W is not None and W.device != K.device):
+            raise ValueError("the tensors of a cache must be on one device")
+        self.K, self.V, self.table, self.lens, self.W = K, V, table, lens, W
+        self.dtype, self.device, self.code = K.dtype, K.device, _dtype_code(K)
+        self.B, self.capacity = table.shape[0], table.shape[1] * self.page_size
+        self.struct = seka_paged(_dev(K, "K"), _dev(V, "V"), _dev(W, "W"), _dev(table, "table"), _dev(lens, "lens"), pages, self.page_size,
+                                 table.shape[1])
+        self.ref = ctypes.byref(self.struct)
+
+
+def paged_cache(K, V, table, lens, W=None):
+    """K, V [num_pages, page_size, Hkv, D]; table [B, max_pages] and lens [B] int32; W [num_pages, Hkv, page_size] fp32 or None."""
+    return PagedCache(K, V, table, lens, W)
+
+
+def _chunk(X, cache, cu_seqlens, heads, name):
+    """Checks of a packed tensor against its cache; returns its pointer."""
+    if X.dim() != 3 or X.shape[2] != cache.D or X.dtype != cache.dtype or (heads is not None and X.shape[1] != heads):
+        raise ValueError(f"{name} must be [total, {'heads' if heads is None else heads}, {cache.D}] of dtype {cache.dtype}")
+    if cu_seqlens.dtype != torch.int32 or cu_seqlens.numel() != cache.B + 1:
+        raise ValueError(f"cu_seqlens must be int32 [B + 1 = {cache.B + 1}]")
+    if X.device != cache.device:
+        raise ValueError(f"{name} must be on the cache's device")
+    return _dev(X, name)
+
+
+def seka_rotary(Q, Q_out, rope, K=None, K_out=None, positions=None, stream=None):
+    """Q/Q_out [B,S,Hq,D], K/K_out [B,S,Hkv,D] or None; outputs may be the inputs.  positions [B,S] int32 device tensor or None."""
+    B, S, Hq, D = Q.shape
+    if Q_out.shape != Q.shape or Q_out.dtype != Q.dtype:
+        raise ValueError("Q_out must be like Q")
+    Hkv = 1
+    if K is not None:
+        if K.shape[:2] != Q.shape[:2] or K.shape[3] != D or K.dtype != Q.dtype or K_out is None or K_out.shape != K.shape or K_out.dtype != K.dtype:
+            raise ValueError("K and K_out must be [B, S, Hkv, D] of Q's dtype")
+        Hkv = K.shape[2]
+    if positions is not None and (positions.dtype != torch.int32 or positions.numel() != B * S):
+        raise ValueError("positions must be int32, one per token")
+    sh = _shape(B, S, Hq, Hkv, D, _dtype_code(Q), 0.0)
+    _check(lib.seka_rotary(_dev(Q, "Q"), _dev(Q_out, "Q_out"), _dev(K, "K"), _dev(K_out, "K_out"), ctypes.byref(sh), rope.ref,
+                           _dev(positions, "positions"), _stream(stream)))
+    return Q_out
+
+
+def seka_cache_append(K, V, cache, cu_seqlens, max_q, rope=None, positions=None, Q=None, Q_out=None, mask=None, max_len=None, stream=None):
+    """K/V [total,Hkv,D] into the pages, turned by rope if given; Q [total,Hq,D] -> Q_out turned beside them.  positions [total]
+    int32 or None (index in the cache); mask [total] uint8 or None; max_len: the most cached tokens (the table's capacity if None)."""
+    total = K.shape[0]
+    k, v = _chunk(K, cache, cu_seqlens, cache.Hkv, "K"), _chunk(V, cache, cu_seqlens, cache.Hkv, "V")
+    Hq = cache.Hkv
+    q = qo = None
+    if Q is not None:
+        Hq = Q.shape[1]
+        q, qo = _chunk(Q, cache, cu_seqlens, Hq, "Q"), _chunk(Q_out, cache, cu_seqlens, Hq, "Q_out")
+    if V.shape[0] != total or (Q is not None and (Q.shape[0] != total or Q_out.shape[0] != total)):
+        raise ValueError("K, V, Q and Q_out must have one row per new token")
+    if positions is not None and (positions.dtype != torch.int32 or positions.numel() != total):
+        raise ValueError("positions must be int32, one per new token")
+    if mask is not None and (mask.dtype != torch.uint8 or mask.numel() != total):
+        raise ValueError("mask must be uint8, one per new token")
+    sh = _shape(cache.B, cache.capacity if max_len is None else max_len, Hq, cache.Hkv, cache.D, cache.code, 0.0)
+    _check(lib.seka_cache_append(k, v, q, qo, ctypes.byref(sh), cache.ref, rope.ref if rope is not None else None, _dev(positions, "positions"),
+                                 _dev(mask, "mask"), _dev(cu_seqlens, "cu_seqlens"), total, max_q, _stream(stream)))
+
+
+def seka_chunk_workspace_bytes(B, S, Hq, Hkv, D, dtype, total_tokens, max_q):
+    sh = _shape(B, S, Hq, Hkv, D, dtype, 0.0)
+    return lib.seka_chunk_workspace_bytes(ctypes.byref(sh), total_tokens, max_q)
+
+
+def seka_attention_chunk(Q, O, cache, cu_seqlens, max_q, max_len=None, lse=None, scale=0.0, workspace=None, stream=None):
+    """Q/O [total,Hq,D]; cu_seqlens [B+1] int32 device tensor; max_q: the longest chunk; max_len: the most cached tokens (the
+    table's capacity if None); lse [Hq,total] fp32 or None."""
+    total, Hq, _ = Q.shape
+    q, o = _chunk(Q, cache, cu_seqlens, Hq, "Q"), _chunk(O, cache, cu_seqlens, Hq, "O")
+    if O.shape[0] != total or (lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (Hq, total))):
+        raise ValueError(f"O must be like Q, lse fp32 [Hq={Hq}, total={total}]")
+    sh = _shape(cache.B, cache.capacity if max_len is None else max_len, Hq, cache.Hkv, cache.D, cache.code, scale)
+    if workspace is None:
+        need = lib.seka_chunk_workspace_bytes(ctypes.byref(sh), total, max_q)
+        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=Q.device)
+    _check(lib.seka_attention_chunk(q, o, _dev(lse, "lse"), ctypes.byref(sh), cache.ref, _dev(cu_seqlens, "cu_seqlens"), total, max_q,
+                                    _dev(workspace, "workspace"), workspace.numel() * workspace.element_size(), _stream(stream)))
+    return O
+
+
+def seka_attention_weights(Q, lse, cache, cu_seqlens, max_q, max_len=None, window=None, W_in=None, decay=1.0, scale=0.0, stream=None):
+    """Writes cache.W: decay * W_in (zeros if None) plus the attention that every cached token gets from the last `window` new
+    tokens (all if None) of every chunk.  Q [total,Hq,D], lse [Hq,total] of seka_attention_chunk."""
+    total, Hq, _ = Q.shape
+    q = _chunk(Q, cache, cu_seqlens, Hq, "Q")
+    if lse.dtype != torch.float32 or tuple(lse.shape) != (Hq, total):
+        raise ValueError(f"lse must be fp32 [Hq={Hq}, total={total}]")
+    if W_in is not None and (cache.W is None or W_in.dtype != torch.float32 or W_in.shape != cache.W.shape):
+        raise ValueError("W_in must be like the cache's W")
+    sh = _shape(cache.B, cache.capacity if max_len is None else max_len, Hq, cache.Hkv, cache.D, cache.code, scale)
+    _check(lib.seka_attention_weights(q, _dev(lse, "lse"), ctypes.byref(sh), cache.ref, _dev(W_in, "W_in"), _dev(cu_seqlens, "cu_seqlens"),
+                                      total, max_q, max_q if window is None else window, float(decay), _stream(stream)))
+    return cache.W
+
+
+def seka_cache_evict(src, dst, kept, recent, lens_out=None, max_len=None, stream=None):
+    """Cuts src's caches to kept.shape[2] tokens per head, into dst's pages (src itself: in place).  kept [B,Hkv,budget] int32;
+    lens_out [B] int32 (dst.lens if None; not src.lens).  Returns lens_out."""
+    if (dst.B, dst.Hkv, dst.D, dst.dtype) != (src.B, src.Hkv, src.D, src.dtype):
+        raise ValueError("src and dst must have the same requests, heads and dtype")
+    if kept.dtype != torch.int32 or kept.dim() != 3 or tuple(kept.shape[:2]) != (src.B, src.Hkv):
+        raise ValueError(f"kept must be int32 [B={src.B}, Hkv={src.Hkv}, budget]")
+    if lens_out is None:
+        lens_out = dst.lens
+    if lens_out.dtype != torch.int32 or lens_out.numel() != src.B:
+        raise ValueError(f"lens_out must be int32 [B={src.B}]")
+    sh = _shape(src.B, src.capacity if max_len is None else max_len, src.Hkv, src.Hkv, src.D, src.code, 0.0)
+    _check(lib.seka_cache_evict(ctypes.byref(sh), src.ref, dst.ref, kept.shape[2], recent, _dev(kept, "kept"), _dev(lens_out, "lens_out"),
+                                _stream(stream)))
+    return lens_out

@@ -4,6 +4,7 @@
 #include <cstring>
 
 #include "common.h"
+#include "paged.h"
 
 namespace {
 
@@ -107,6 +108,59 @@ seka_status attention_common(const void* Q, const void* K, const void* V, void* 
                      : seka::launch_attention_f32(a, steered ? &sa : nullptr, stream);
   return launch_status(e);
 }
+
+// ---- caches of pages ----
+constexpr double kTwoPi = 6.283185307179586476925286766559;
+
+size_t pool_bytes(const seka_paged* c, const seka_shape* sh) {
+  return (size_t)c->num_pages * c->page_size * sh->Hkv * sh->D * elem_size(sh->dtype);
+}
+size_t pool_weight_bytes(const seka_paged* c, const seka_shape* sh) { return (size_t)c->num_pages * c->page_size * sh->Hkv * sizeof(float); }
+
+seka_status check_paged(const seka_paged* c, const seka_shape* sh, bool need_w, bool need_lens) {
+  if (!c || !c->K || !c->V || !c->table || (need_lens && !c->lens) || (need_w && !c->W)) return SEKA_ERR_NULL;
+  if (c->num_pages < 1 || c->max_pages < 1) return SEKA_ERR_SHAPE;
+  if (c->page_size < 8 || c->page_size > 65536 || (c->page_size & (c->page_size - 1))) return SEKA_ERR_SHAPE;
+  if (sh->B > kMaxGridYZ) return SEKA_ERR_SHAPE;
+  if (misaligned(c->K) || misaligned(c->V) || (c->W && misaligned(c->W))) return SEKA_ERR_ALIGN;
+  if ((reinterpret_cast<uintptr_t>(c->table) & 3u) || (c->lens && (reinterpret_cast<uintptr_t>(c->lens) & 3u))) return SEKA_ERR_ALIGN;
+  return SEKA_OK;
+}
+
+seka::PagedCache paged(const seka_paged* c, const seka_shape* sh) {
+  seka::PagedCache p;
+  p.K = c->K; p.V = c->V; p.W = c->W; p.table = c->table; p.lens = c->lens;
+  p.num_pages = c->num_pages; p.max_pages = c->max_pages;
+  p.shift = 0;
+  while ((1 << p.shift) < c->page_size) ++p.shift;
+  const int64_t room = (int64_t)c->max_pages * c->page_size;
+  p.cap = (int)(room < sh->S ? room : sh->S);
+  return p;
+}
+
+// New tokens of a call; max_q is what a kernel may take for the longest chunk.
+seka_status check_chunk(const int32_t* cu, int64_t total, int32_t max_q, const seka_shape* sh, seka::ChunkRows* r) {
+  if (!cu) return SEKA_ERR_NULL;
+  if (reinterpret_cast<uintptr_t>(cu) & 3u) return SEKA_ERR_ALIGN;
+  if (total < 1 || total > 0x7fffffffLL || max_q < 1 || max_q > sh->S) return SEKA_ERR_SHAPE;
+  r->cu = cu; r->B = sh->B; r->total = (int)total; r->max_q = max_q;
+  return SEKA_OK;
+}
+
+seka_status check_rope(const seka_rope* rope, const seka_shape* sh, seka::RotaryArgs* a) {
+  if (!rope->freq) return SEKA_ERR_NULL;
+  if (rope->dim < 2 || rope->dim > sh->D || rope->dim % 2 || !std::isfinite(rope->factor)) return SEKA_ERR_SHAPE;
+  for (int i = 0; i < rope->dim / 2; ++i) {
+    if (!std::isfinite(rope->freq[i])) return SEKA_ERR_SHAPE;
+    a->turns[i] = rope->freq[i] / kTwoPi;
+  }
+  a->half = rope->dim / 2;
+  a->interleaved = rope->interleaved != 0;
+  a->factor = rope->factor == 0.0f ? 1.0f : rope->factor;
+  return SEKA_OK;
+}
+
+float scale_of(const seka_shape* sh) { return sh->softmax_scale > 0.0f ? sh->softmax_scale : 1.0f / std::sqrt((float)sh->D); }
 
 }  // namespace
 
@@ -396,6 +450,175 @@ seka_status seka_attention_prefill_packed(const void* Q, const void* K, const vo
                                           int64_t total_tokens, void* hip_stream) {
   if (!cu_seqlens) return SEKA_ERR_NULL;
   return attention_common(Q, K, V, O, lse, sh, st, nullptr, cu_seqlens, total_tokens, hip_stream);
+}
+
+seka_status seka_rope_frequencies(int32_t dim, double base, int32_t scaling, double stretch, double original, double fast,
+                                  double slow, double* freq_out) {
+  if (!freq_out) return SEKA_ERR_NULL;
+  if (dim < 2 || dim % 2 || dim > 128 || !std::isfinite(base) || !(base > 1.0)) return SEKA_ERR_SHAPE;
+  if (scaling < SEKA_ROPE_PLAIN || scaling > SEKA_ROPE_TURNS) return SEKA_ERR_UNSUPPORTED;
+  if (scaling != SEKA_ROPE_PLAIN && (!std::isfinite(stretch) || !(stretch >= 1.0))) return SEKA_ERR_SHAPE;
+  const bool parts = scaling == SEKA_ROPE_PARTS || scaling == SEKA_ROPE_TURNS;
+  if (parts && !(std::isfinite(original) && original > 0.0 && std::isfinite(fast) && slow > 0.0 && fast > slow)) return SEKA_ERR_SHAPE;
+  if (scaling == SEKA_ROPE_BASE && dim == 2) return SEKA_ERR_SHAPE;      // its only pair has frequency 1 whatever the base
+  if (scaling == SEKA_ROPE_BASE) base *= std::pow(stretch, (double)dim / (dim - 2));
+  const auto pair_of = [&](double turns) { return dim * std::log(original / (kTwoPi * turns)) / (2.0 * std::log(base)); };
+  const double lo = parts ? std::fmax(std::floor(pair_of(fast)), 0.0) : 0.0;
+  const double hi = parts ? std::fmin(std::ceil(pair_of(slow)), (double)dim - 1) : 0.0;
+  for (int i = 0; i < dim / 2; ++i) {
+    const double f = std::pow(base, -2.0 * i / dim);
+    double stretched = 0.0;                // share of f / stretch
+    if (scaling == SEKA_ROPE_LINEAR) stretched = 1.0;
+    if (scaling == SEKA_ROPE_PARTS) stretched = (i - lo) / std::fmax(hi - lo, 1e-3);
+    if (scaling == SEKA_ROPE_TURNS) stretched = (fast - original * f / kTwoPi) / (fast - slow);
+    stretched = std::fmin(std::fmax(stretched, 0.0), 1.0);
+    freq_out[i] = f * (1.0 - stretched) + f / (scaling == SEKA_ROPE_PLAIN ? 1.0 : stretch) * stretched;
+  }
+  return SEKA_OK;
+}
+
+seka_status seka_rotary(const void* Q, void* Q_out, const void* K, void* K_out, const seka_shape* sh, const seka_rope* rope,
+                        const int32_t* positions, void* hip_stream) {
+  seka_status rc = check_shape(sh, true);
+  if (rc != SEKA_OK) return rc;
+  if (!Q || !Q_out || !rope || (K == nullptr) != (K_out == nullptr)) return SEKA_ERR_NULL;
+  seka::RotaryArgs a = {};
+  if ((rc = check_rope(rope, sh, &a)) != SEKA_OK) return rc;
+  const int64_t total = (int64_t)sh->B * sh->S;
+  if (total > 0x7fffffffLL) return SEKA_ERR_SHAPE;
+  if (misaligned(Q) || misaligned(Q_out) || misaligned(K) || misaligned(K_out) || (reinterpret_cast<uintptr_t>(positions) & 3u)) return SEKA_ERR_ALIGN;
+  const size_t nq = (size_t)total * sh->Hq * sh->D * elem_size(sh->dtype), nk = K ? (size_t)total * sh->Hkv * sh->D * elem_size(sh->dtype) : 0;
+  if ((Q_out != Q && ranges_overlap(Q_out, nq, Q, nq)) ||
+      (K && ((K_out != K && ranges_overlap(K_out, nk, K, nk)) || ranges_overlap(Q_out, nq, K, nk) || ranges_overlap(K_out, nk, Q, nq) ||
+             ranges_overlap(Q_out, nq, K_out, nk))))
+    return SEKA_ERR_ALIAS;
+  if (positions && (ranges_overlap(Q_out, nq, positions, (size_t)total * 4) || (K && ranges_overlap(K_out, nk, positions, (size_t)total * 4)))) return SEKA_ERR_ALIAS;
+  a.Q = Q; a.Q_out = Q_out; a.K = K; a.K_out = K_out; a.positions = positions;
+  a.total = (int)total; a.S = sh->S; a.Hq = sh->Hq; a.Hkv = sh->Hkv; a.D = sh->D;
+  (void)hipGetLastError();
+  return launch_status(seka::launch_rotary(a, sh->dtype, reinterpret_cast<hipStream_t>(hip_stream)));
+}
+
+seka_status seka_cache_append(const void* K, const void* V, const void* Q, void* Q_out, const seka_shape* sh,
+                              const seka_paged* cache, const seka_rope* rope, const int32_t* positions, const uint8_t* mask,
+                              const int32_t* cu_seqlens, int64_t total_tokens, int32_t max_q, void* hip_stream) {
+  seka_status rc = check_shape(sh, true);
+  if (rc != SEKA_OK) return rc;
+  if ((rc = check_paged(cache, sh, false, true)) != SEKA_OK) return rc;
+  if (!K || !V || (Q == nullptr) != (Q_out == nullptr)) return SEKA_ERR_NULL;
+  seka::RotaryArgs a = {};
+  if ((rc = check_chunk(cu_seqlens, total_tokens, max_q, sh, &a.r)) != SEKA_OK) return rc;
+  if (rope) {
+    if ((rc = check_rope(rope, sh, &a)) != SEKA_OK) return rc;
+  } else if (Q) {
+    return SEKA_ERR_UNSUPPORTED;           // nothing to do to the queries
+  }
+  if (misaligned(K) || misaligned(V) || misaligned(Q) || misaligned(Q_out) || (reinterpret_cast<uintptr_t>(positions) & 3u)) return SEKA_ERR_ALIGN;
+  const size_t es = elem_size(sh->dtype), pool = pool_bytes(cache, sh);
+  const size_t nq = Q ? (size_t)total_tokens * sh->Hq * sh->D * es : 0, nk = (size_t)total_tokens * sh->Hkv * sh->D * es;
+  const void* outs[4] = {cache->K, cache->V, cache->W, Q_out};
+  const size_t out_bytes[4] = {pool, pool, cache->W ? pool_weight_bytes(cache, sh) : 0, nq};
+  const size_t entries = (size_t)sh->B * cache->max_pages * 4;
+  const void* ins[7] = {K, V, Q, positions, mask, cache->table, cache->lens};
+  const size_t in_bytes[7] = {nk, nk, nq, positions ? (size_t)total_tokens * 4 : 0, mask ? (size_t)total_tokens : 0, entries, (size_t)sh->B * 4};
+  for (int i = 0; i < 4; ++i) {
+    if (!out_bytes[i]) continue;
+    for (int j = 0; j < 7; ++j)
+      if (in_bytes[j] && !(i == 3 && j == 2 && Q_out == Q) && ranges_overlap(outs[i], out_bytes[i], ins[j], in_bytes[j])) return SEKA_ERR_ALIAS;
+    for (int j = i + 1; j < 4; ++j)
+      if (out_bytes[j] && ranges_overlap(outs[i], out_bytes[i], outs[j], out_bytes[j])) return SEKA_ERR_ALIAS;
+  }
+  a.Q = Q; a.Q_out = Q_out; a.K = K; a.V = V; a.positions = positions; a.mask = mask;
+  a.c = paged(cache, sh);
+  a.total = (int)total_tokens; a.S = sh->S; a.Hq = sh->Hq; a.Hkv = sh->Hkv; a.D = sh->D;
+  (void)hipGetLastError();
+  return launch_status(seka::launch_rotary(a, sh->dtype, reinterpret_cast<hipStream_t>(hip_stream)));
+}
+
+size_t seka_chunk_workspace_bytes(const seka_shape* sh, int64_t total_tokens, int32_t max_q) {
+  if (check_shape(sh, true) != SEKA_OK || sh->B > kMaxGridYZ || total_tokens < 1 || total_tokens > 0x7fffffffLL || max_q < 1 || max_q > sh->S) return 0;
+  return seka::chunk_workspace_bytes(sh->B, sh->S, sh->Hq, sh->Hkv, sh->D, sh->dtype, (int)total_tokens, max_q);
+}
+
+seka_status seka_attention_chunk(const void* Q, void* O, float* lse, const seka_shape* sh, const seka_paged* cache,
+                                 const int32_t* cu_seqlens, int64_t total_tokens, int32_t max_q, void* workspace,
+                                 size_t workspace_bytes, void* hip_stream) {
+  seka_status rc = check_shape(sh, true);
+  if (rc != SEKA_OK) return rc;
+  if ((rc = check_paged(cache, sh, false, true)) != SEKA_OK) return rc;
+  if (!Q || !O) return SEKA_ERR_NULL;
+  seka::ChunkArgs a = {};
+  if ((rc = check_chunk(cu_seqlens, total_tokens, max_q, sh, &a.r)) != SEKA_OK) return rc;
+  if (misaligned(Q) || misaligned(O) || (reinterpret_cast<uintptr_t>(lse) & 3u)) return SEKA_ERR_ALIGN;
+  const size_t nq = (size_t)total_tokens * sh->Hq * sh->D * elem_size(sh->dtype), pool = pool_bytes(cache, sh);
+  const size_t nl = lse ? (size_t)total_tokens * sh->Hq * sizeof(float) : 0;
+  if (ranges_overlap(O, nq, Q, nq) || ranges_overlap(O, nq, cache->K, pool) || ranges_overlap(O, nq, cache->V, pool)) return SEKA_ERR_ALIAS;
+  if (lse && (ranges_overlap(lse, nl, O, nq) || ranges_overlap(lse, nl, Q, nq) || ranges_overlap(lse, nl, cache->K, pool) || ranges_overlap(lse, nl, cache->V, pool)))
+    return SEKA_ERR_ALIAS;
+  const size_t need = seka::chunk_workspace_bytes(sh->B, sh->S, sh->Hq, sh->Hkv, sh->D, sh->dtype, (int)total_tokens, max_q);
+  if (need && (!workspace || workspace_bytes < need)) return SEKA_ERR_WORKSPACE;
+  if (misaligned(workspace)) return SEKA_ERR_ALIGN;
+  a.Q = Q; a.O = O; a.lse = lse; a.c = paged(cache, sh);
+  a.part = static_cast<float*>(workspace);
+  a.Hq = sh->Hq; a.Hkv = sh->Hkv; a.scale = scale_of(sh);
+  (void)hipGetLastError();
+  return launch_status(seka::launch_chunk(a, sh->D, sh->dtype, sh->S, reinterpret_cast<hipStream_t>(hip_stream)));
+}
+
+seka_status seka_attention_weights(const void* Q, const float* lse, const seka_shape* sh, const seka_paged* cache,
+                                   const float* W_in, const int32_t* cu_seqlens, int64_t total_tokens, int32_t max_q,
+                                   int32_t window, float decay, void* hip_stream) {
+  seka_status rc = check_shape(sh, true);
+  if (rc != SEKA_OK) return rc;
+  if ((rc = check_paged(cache, sh, true, true)) != SEKA_OK) return rc;
+  if (!Q || !lse) return SEKA_ERR_NULL;
+  seka::WeightsArgs a = {};
+  if ((rc = check_chunk(cu_seqlens, total_tokens, max_q, sh, &a.r)) != SEKA_OK) return rc;
+  if (window < 1 || !std::isfinite(decay)) return SEKA_ERR_SHAPE;
+  if (misaligned(Q) || (reinterpret_cast<uintptr_t>(lse) & 3u) || misaligned(W_in)) return SEKA_ERR_ALIGN;
+  const size_t nw = pool_weight_bytes(cache, sh), pool = pool_bytes(cache, sh);
+  const size_t nq = (size_t)total_tokens * sh->Hq * sh->D * elem_size(sh->dtype), nl = (size_t)total_tokens * sh->Hq * sizeof(float);
+  if (ranges_overlap(cache->W, nw, Q, nq) || ranges_overlap(cache->W, nw, lse, nl) || ranges_overlap(cache->W, nw, cache->K, pool) ||
+      (W_in && W_in != cache->W && ranges_overlap(cache->W, nw, W_in, nw)))
+    return SEKA_ERR_ALIAS;
+  a.Q = Q; a.lse = lse; a.W_in = decay != 0.0f ? W_in : nullptr; a.c = paged(cache, sh);
+  a.Hq = sh->Hq; a.Hkv = sh->Hkv; a.window = window; a.scale = scale_of(sh); a.decay = decay;
+  (void)hipGetLastError();
+  return launch_status(seka::launch_weights(a, sh->D, sh->dtype, reinterpret_cast<hipStream_t>(hip_stream)));
+}
+
+seka_status seka_cache_evict(const seka_shape* sh, const seka_paged* src, const seka_paged* dst, int32_t budget, int32_t recent,
+                             int32_t* kept, int32_t* lens_out, void* hip_stream) {
+  seka_status rc = check_shape(sh, false);
+  if (rc != SEKA_OK) return rc;
+  if ((rc = check_paged(src, sh, true, true)) != SEKA_OK) return rc;
+  if ((rc = check_paged(dst, sh, true, false)) != SEKA_OK) return rc;
+  if (!kept || !lens_out) return SEKA_ERR_NULL;
+  if (budget < 1 || recent < 0 || recent > budget) return SEKA_ERR_SHAPE;
+  if ((int64_t)dst->max_pages * dst->page_size < (budget < sh->S ? budget : sh->S)) return SEKA_ERR_SHAPE;
+  if ((reinterpret_cast<uintptr_t>(kept) & 3u) || (reinterpret_cast<uintptr_t>(lens_out) & 3u)) return SEKA_ERR_ALIGN;
+  // a tensor of dst is the same tensor of src or overlaps nothing of it
+  const bool same = dst->K == src->K || dst->V == src->V || dst->W == src->W;
+  if (same && (dst->K != src->K || dst->V != src->V || dst->W != src->W || dst->num_pages != src->num_pages || dst->page_size != src->page_size))
+    return SEKA_ERR_ALIAS;
+  const void* t[8] = {src->K, src->V, src->W, dst->K, dst->V, dst->W, kept, lens_out};
+  const size_t n[8] = {pool_bytes(src, sh), pool_bytes(src, sh), pool_weight_bytes(src, sh), pool_bytes(dst, sh), pool_bytes(dst, sh),
+                       pool_weight_bytes(dst, sh), (size_t)sh->B * sh->Hkv * budget * 4, (size_t)sh->B * 4};
+  for (int i = 0; i < 8; ++i)
+    for (int j = i + 1; j < 8; ++j)
+      if (!(same && j == i + 3 && j < 6) && ranges_overlap(t[i], n[i], t[j], n[j])) return SEKA_ERR_ALIAS;
+  const void* tables[3] = {src->table, dst->table, src->lens};
+  const size_t nt[3] = {(size_t)sh->B * src->max_pages * 4, (size_t)sh->B * dst->max_pages * 4, (size_t)sh->B * 4};
+  for (int i = 0; i < 3; ++i)
+    for (int j = 3; j < 8; ++j)
+      if (ranges_overlap(tables[i], nt[i], t[j], n[j])) return SEKA_ERR_ALIAS;
+  seka::EvictArgs a = {};
+  a.src = paged(src, sh);
+  a.dst = paged(dst, sh);
+  a.kept = kept; a.lens_out = lens_out;
+  a.B = sh->B; a.Hkv = sh->Hkv; a.row_bytes = sh->D * (int)elem_size(sh->dtype); a.budget = budget; a.recent = recent;
+  (void)hipGetLastError();
+  return launch_status(seka::launch_evict(a, reinterpret_cast<hipStream_t>(hip_stream)));
 }
 
 }  // extern "C"

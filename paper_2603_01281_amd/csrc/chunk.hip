@@ -1,0 +1,251 @@
+// seka_attention_chunk: new tokens of a batch of requests attend to their caches of pages, bf16.
+//
+//   s_ij = scale q_i . k_j for j <= len - n + i;   O_i = sum_j softmax(s_i)_j v_j;   lse_i = log sum_j exp(s_ij)
+//
+// Rows: new token i and head g of a KV head's group are row i G + g, so that all of a group's queries share every key read.
+// A workgroup takes R = 16 RT rows of one request and KV head and a range of its keys (paged.h, plan_item); its four waves take
+// 32-key blocks in turn and never synchronise before they merge.
+//   S^T (keys x rows)  = K q^T       A = K rows from LDS, B = queries in registers
+//   O^T (D x rows)    += V^T P^T     A = V^T by transposing LDS reads, B = P^T straight from the S^T accumulators
+// Keys and values are fetched as whole rows into registers, a block ahead, and pass through a wave-private LDS tile.
+#include <algorithm>
+
+#include "chunk_rows.h"
+
+namespace seka {
+namespace {
+
+typedef __attribute__((address_space(3))) s16x4* row_lds_s16x4_ptr;
+typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
+
+template <int D, int RT>
+__global__ __launch_bounds__(kRowThreads, 2) void chunk_rows_bf16_kernel(ChunkArgs a) {
+  constexpr int BK = 32, R = 16 * RT;
+  // LDS row strides (elements): 16 rows of K at one 16-byte column, and 16 rows x 32 bytes of V, spread over all banks
+  constexpr int LDK = D + 8, LDV = D + 16, OLD = D + 4;
+  constexpr int KS = D / 32, DT = D / 16;
+  constexpr int CPR = D / 8, RPI = 64 / CPR, NV = BK / RPI;     // 16-byte pieces per row, rows per load, loads per block
+  constexpr int kTileBytes = BK * LDV * 2, kMergeBytes = 16 * OLD * 4;
+  constexpr int kAreaBytes = kTileBytes > kMergeBytes ? kTileBytes : kMergeBytes;
+  __shared__ __attribute__((aligned(16))) unsigned char smem[kRowWaves * kAreaBytes];
+  __shared__ float sm_ml[kRowWaves][16][2];
+
+  ChunkItem it;
+  if (!plan_item<false>(a.r, a.c, a.p, blockIdx.x, it)) return;         // workgroup-uniform
+  int k0, k1;
+  plan_range(a.p, it, k0, k1);
+  const int h = blockIdx.y, G = a.p.G;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, grp = lane >> 4;
+  const int nrows = it.e.n * G, ctx = it.e.len - it.e.n;
+  uint16_t* tile = reinterpret_cast<uint16_t*>(smem + wave * kAreaBytes);
+
+  // ---- queries: lane (row 16 rt + l16, d = 32 ks + 8 grp ..) ----
+  bf16x8 qf[RT][KS];
+  int last[RT];                            // last key that this lane's row sees
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const int row = it.rc * R + 16 * rt + l16;
+    const bool ok = row < nrows;
+    const int i = ok ? row / G : 0, g = ok ? row % G : 0;
+    last[rt] = ok ? ctx + i : -1;
+    const uint16_t* qp = static_cast<const uint16_t*>(a.Q) + ((size_t)(it.e.row0 + i) * a.Hq + h * G + g) * D + 8 * grp;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      u32x4 v = {0, 0, 0, 0};
+      if (ok) v = *reinterpret_cast<const u32x4*>(qp + 32 * ks);
+      qf[rt][ks] = __builtin_bit_cast(bf16x8, v);
+    }
+  }
+  const int all_see = ctx + it.rc * R / G; // keys up to here are seen by every row
+
+  float m[RT], l[RT];
+  f32x4 o[DT][RT];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    m[rt] = kRowLow;
+    l[rt] = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) o[dt][rt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  const float c2 = a.scale * 1.4426950408889634f;
+
+  const uint32_t row_bytes = (uint32_t)a.Hkv * D * 2;
+  const uint32_t lane_off = (uint32_t)(lane / CPR) * row_bytes + 16u * (lane % CPR);
+  const char* Kh = static_cast<const char*>(a.c.K) + (size_t)h * D * 2;
+  const char* Vh = static_cast<const char*>(a.c.V) + (size_t)h * D * 2;
+  const int slots = (1 << a.c.shift) - 1;
+  u32x4 kr[NV], vr[NV];
+  PageWindow<BK> win;
+  int block = 0;                           // of the window
+  auto fetch = [&](int kb) __attribute__((always_inline)) {
+    if (block == win.left) {
+      win.load(a.c, it.b, kb, k1);
+      block = 0;
+    }
+    const int at = block * win.per_block;
+    ++block;
+    if (kb + BK <= k1) {
+#pragma unroll
+      for (int x = 0; x < NV; ++x) {       // the RPI <= 8 rows of a load lie in one page
+        const int page = __builtin_amdgcn_readlane(win.entry, at + (win.per_block > 1 ? (RPI * x) >> a.c.shift : 0));
+        const size_t off = (((size_t)page << a.c.shift) + ((kb + RPI * x) & slots)) * row_bytes;
+        kr[x] = *reinterpret_cast<const u32x4*>(Kh + off + lane_off);
+        vr[x] = *reinterpret_cast<const u32x4*>(Vh + off + lane_off);
+      }
+    } else {                               // rows behind the last key repeat it
+#pragma unroll
+      for (int x = 0; x < NV; ++x) {
+        const int key = min(kb + RPI * x + lane / CPR, k1 - 1);
+        const int page = __shfl(win.entry, at + (win.per_block > 1 ? (key - kb) >> a.c.shift : 0));
+        const size_t off = (((size_t)page << a.c.shift) + (key & slots)) * row_bytes + 16u * (lane % CPR);
+        kr[x] = *reinterpret_cast<const u32x4*>(Kh + off);
+        vr[x] = *reinterpret_cast<const u32x4*>(Vh + off);
+      }
+    }
+  };
+
+  int kb = k0 + wave * BK;
+  if (kb < k1) {
+    win.load(a.c, it.b, kb, k1);
+    fetch(kb);
+  }
+  for (; kb < k1; kb += kRowWaves * BK) {
+    // (a wave's LDS operations execute in program order; the fences are for the compiler)
+#pragma unroll
+    for (int x = 0; x < NV; ++x) *reinterpret_cast<u32x4*>(tile + (RPI * x + lane / CPR) * LDK + 8 * (lane % CPR)) = kr[x];
+    asm volatile("" ::: "memory");
+    f32x4 sc[2][RT];
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) sc[kt][rt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt) {
+        const bf16x8 kf = *reinterpret_cast<const bf16x8*>(tile + (16 * kt + l16) * LDK + 32 * ks + 8 * grp);
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) sc[kt][rt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[rt][ks], sc[kt][rt], 0, 0, 0);
+      }
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int x = 0; x < NV; ++x) *reinterpret_cast<u32x4*>(tile + (RPI * x + lane / CPR) * LDV + 8 * (lane % CPR)) = vr[x];
+    asm volatile("" ::: "memory");
+    const int kb_next = kb + kRowWaves * BK;
+    if (kb_next < k1) fetch(kb_next);      // on their way during the softmax
+
+    bf16x8 pb[RT];
+    const bool masked = kb + BK - 1 > all_see || kb + BK > k1;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      float t[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) t[e] = sc[e >> 2][rt][e & 3] * c2;
+      if (masked) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (kb + 16 * (e >> 2) + 4 * grp + (e & 3) > last[rt]) t[e] = -INFINITY;
+      }
+      float top = t[0];
+#pragma unroll
+      for (int e = 1; e < 8; ++e) top = fmaxf(top, t[e]);
+      top = groups_max(top);
+      const bool raise = top > m[rt] + kRowSlack;
+      if (__any(raise)) {                  // rare behind the first blocks
+        const float f = raise ? __builtin_amdgcn_exp2f(m[rt] - top) : 1.f;
+        if (raise) m[rt] = top;
+        l[rt] *= f;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) o[dt][rt] *= f;
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float p = __builtin_amdgcn_exp2f(t[e] - m[rt]);
+        l[rt] += p;                        // of the probabilities before their rounding
+        pb[rt][e] = (__bf16)p;
+      }
+    }
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      // lane: d = 16 dt + l16, slot e <-> key 16 (e / 4) + 4 grp + e % 4, as in the score accumulators
+      const uint16_t* p = tile + (4 * grp + (l16 >> 2)) * LDV + 16 * dt + 4 * (l16 & 3);
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((row_lds_s16x4_ptr)(p));
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((row_lds_s16x4_ptr)(p + 16 * LDV));
+      const bf16x8 vf = __builtin_shufflevector(__builtin_bit_cast(bf16x4, lo), __builtin_bit_cast(bf16x4, hi), 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) o[dt][rt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pb[rt], o[dt][rt], 0, 0, 0);
+    }
+    asm volatile("" ::: "memory");         // the tile is rewritten behind these reads
+  }
+
+  // ---- merge the waves, 16 rows at a time; lane (row l16, grp) holds O[row][16 dt + 4 grp + i] ----
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const float lt = groups_sum(l[rt]);
+    __syncthreads();                       // the tiles, or the merge area of the rows before, are free
+    float* mo = reinterpret_cast<float*>(smem) + wave * 16 * OLD;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f32x4*>(mo + l16 * OLD + 16 * dt + 4 * grp) = o[dt][rt];
+    if (grp == 0) {
+      sm_ml[wave][l16][0] = m[rt];
+      sm_ml[wave][l16][1] = lt;
+    }
+    __syncthreads();
+    merge_waves<uint16_t, D>(a, it, h, it.rc * R + 16 * rt, reinterpret_cast<const float*>(smem), sm_ml);
+  }
+}
+
+template <int D>
+hipError_t launch_rows(const ChunkArgs& a, int rows16, int items, int chunks, hipStream_t s) {
+  const dim3 grid(items, a.Hkv), block(kRowThreads);
+  if (rows16 == 1) hipLaunchKernelGGL((chunk_rows_bf16_kernel<D, 1>), grid, block, 0, s, a);
+  else if (rows16 == 2) hipLaunchKernelGGL((chunk_rows_bf16_kernel<D, 2>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((chunk_rows_bf16_kernel<D, 4>), grid, block, 0, s, a);
+  if (a.p.max_splits > 1) hipLaunchKernelGGL((chunk_merge_kernel<uint16_t, D>), dim3(chunks, a.Hkv), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+// Rows per workgroup, ranges and the bounds of both, from what the host knows: B requests, `total` new tokens of which no request
+// has more than max_q, caches of up to S tokens.
+struct RowPlan {
+  ChunkPlan p;
+  int rows16, chunks, items;
+};
+RowPlan row_plan(int B, int S, int Hq, int Hkv, int dtype, int total, int max_q) {
+  RowPlan r;
+  const int G = Hq / Hkv;
+  const long long rows = (long long)std::min(max_q, total) * G;
+  r.rows16 = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+  r.p.R = 16 * r.rows16;
+  r.p.G = G;
+  r.chunks = (int)std::min(((long long)total * G) / r.p.R + B, (long long)0x3fffffff);
+  // two workgroups of four waves to a compute unit, about
+  r.p.slots_log2 = 0;
+  while ((1 << r.p.slots_log2) * Hkv < 512) ++r.p.slots_log2;
+  r.p.least = 8;                           // 256 tokens
+  const int blocks = (S + 31) / 32;
+  r.p.max_splits = std::max(1, std::min(64, (blocks + r.p.least - 1) / r.p.least));
+  // sum over chunks of ceil(blocks / L) <= T / L + chunks with T / L <= slots, and no more than every chunk in all its ranges
+  r.items = (int)std::min((long long)r.chunks + (1 << r.p.slots_log2), (long long)r.chunks * r.p.max_splits);
+  return r;
+}
+
+}  // namespace
+
+hipError_t launch_chunk_bf16(const ChunkArgs& a, int D, int rows16, int items, int chunks, hipStream_t s) {
+  return D == 128 ? launch_rows<128>(a, rows16, items, chunks, s) : launch_rows<64>(a, rows16, items, chunks, s);
+}
+
+size_t chunk_workspace_bytes(int B, int S, int Hq, int Hkv, int D, int dtype, int total, int max_q) {
+  const RowPlan r = row_plan(B, S, Hq, Hkv, dtype, total, max_q);
+  return r.p.max_splits > 1 ? (size_t)r.items * Hkv * r.p.R * (D + 4) * sizeof(float) : 0;
+}
+
+hipError_t launch_chunk(ChunkArgs a, int D, int dtype, int S, hipStream_t s) {
+  const RowPlan r = row_plan(a.r.B, S, a.Hq, a.Hkv, dtype, a.r.total, a.r.max_q);
+  a.p = r.p;
+  a.items = r.items;
+  return dtype == SEKA_BF16 ? launch_chunk_bf16(a, D, r.rows16, r.items, r.chunks, s) : launch_chunk_f32(a, D, r.rows16, r.items, r.chunks, s);
+}
+
+}  // namespace seka

@@ -1,0 +1,189 @@
+// seka_attention_chunk, fp32: products and accumulation on v_mfma_f32_16x16x4_f32.
+//
+// Rows, ranges and merging as in the bf16 kernel (chunk.hip).  A wave's step is 16 keys:
+//   S^T (16 keys x 16 rows) = K q^T        lane (row l16, group g) gets keys 4 g + i,
+//   O^T (D x 16 rows)      += V^T P^T      for which it has the operand, and ends with d = 64 hh + 16 g + 4 i + x.
+// K and V go from the pages straight into operand registers with 16-byte loads, those of the wave's next 16 keys as soon as its
+// products with these are issued.  A score is shared by several accumulators: short chains of sums, and no product waits for
+// the one before it.
+#include "chunk_rows.h"
+
+namespace seka {
+namespace {
+
+template <int D, int RT>
+__global__ __launch_bounds__(kRowThreads, RT == 4 ? 1 : 2) void chunk_rows_f32_kernel(ChunkArgs a) {
+  constexpr int NCH = RT == 1 ? 8 : RT == 2 ? 4 : 2;
+  constexpr int KI = D / 16, VH = D / 64, DX = D / 16;
+  constexpr int BK = 16, OLD = D + 4, R = 16 * RT;
+  __shared__ __attribute__((aligned(16))) float sm_o[kRowWaves * 16 * OLD];
+  __shared__ float sm_ml[kRowWaves][16][2];
+
+  ChunkItem it;
+  if (!plan_item<false>(a.r, a.c, a.p, blockIdx.x, it)) return;         // workgroup-uniform
+  int k0, k1;
+  plan_range(a.p, it, k0, k1);
+  const int h = blockIdx.y, G = a.p.G;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, g = lane >> 4;
+  const int nrows = it.e.n * G, ctx = it.e.len - it.e.n;
+
+  f32x4 qv[RT][KI];                        // d = 16 i + 4 g + e
+  int last[RT];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const int row = it.rc * R + 16 * rt + l16;
+    const bool ok = row < nrows;
+    const int i = ok ? row / G : 0, hd = ok ? row % G : 0;
+    last[rt] = ok ? ctx + i : -1;
+    const float* qp = static_cast<const float*>(a.Q) + ((size_t)(it.e.row0 + i) * a.Hq + h * G + hd) * D + 4 * g;
+#pragma unroll
+    for (int x = 0; x < KI; ++x) {
+      qv[rt][x] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (ok) qv[rt][x] = *reinterpret_cast<const f32x4*>(qp + 16 * x);
+    }
+  }
+  const int all_see = ctx + it.rc * R / G;
+
+  const size_t row_floats = (size_t)a.Hkv * D;
+  const float* Kh = static_cast<const float*>(a.c.K) + (size_t)h * D + 4 * g;
+  const float* Vh = static_cast<const float*>(a.c.V) + (size_t)h * D + 4 * l16;
+  const int slots = (1 << a.c.shift) - 1;
+  PageWindow<BK> win;
+  int block = 0, at = 0;
+  f32x4 kv[KI], vv[4][VH];
+  auto turn_window = [&](int kb) __attribute__((always_inline)) {
+    if (block == win.left) {
+      win.load(a.c, it.b, kb, k1);
+      block = 0;
+    }
+    at = block * win.per_block;
+    ++block;
+  };
+  auto row_of = [&](int kb, int key) __attribute__((always_inline)) -> size_t {
+    const int page = __shfl(win.entry, at + (win.per_block > 1 ? (key - kb) >> a.c.shift : 0));
+    return (((size_t)page << a.c.shift) + (key & slots)) * row_floats;
+  };
+  auto fetch_k = [&](int kb) __attribute__((always_inline)) {
+    const float* kp = Kh + row_of(kb, min(kb + l16, k1 - 1));
+#pragma unroll
+    for (int x = 0; x < KI; ++x) kv[x] = *reinterpret_cast<const f32x4*>(kp + 16 * x);
+  };
+  auto fetch_v = [&](int kb) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float* vp = Vh + row_of(kb, min(kb + 4 * g + i, k1 - 1));
+#pragma unroll
+      for (int hh = 0; hh < VH; ++hh) vv[i][hh] = *reinterpret_cast<const f32x4*>(vp + 64 * hh);
+    }
+  };
+
+  f32x4 o[RT][DX];
+  float m[RT], l[RT];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    m[rt] = kRowLow;
+    l[rt] = 0.f;
+#pragma unroll
+    for (int x = 0; x < DX; ++x) o[rt][x] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  const float c2 = a.scale * 1.4426950408889634f;
+  constexpr int TURN = kRowWaves * BK;
+  int kb = k0 + wave * BK;
+  if (kb < k1) {
+    win.load(a.c, it.b, kb, k1);
+    turn_window(kb);
+    fetch_k(kb);
+    fetch_v(kb);
+  }
+  for (; kb < k1; kb += TURN) {
+    const bool more = kb + TURN < k1;
+    f32x4 t[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      f32x4 acc[NCH];
+#pragma unroll
+      for (int c = 0; c < NCH; ++c) acc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int x = 0; x < KI; ++x)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[(4 * x + e) % NCH] = __builtin_amdgcn_mfma_f32_16x16x4f32(kv[x][e], qv[rt][x][e], acc[(4 * x + e) % NCH], 0, 0, 0);
+#pragma unroll
+      for (int half = NCH / 2; half; half /= 2)
+#pragma unroll
+        for (int c = 0; c < half; ++c) acc[c] += acc[c + half];
+      t[rt] = acc[0] * c2;
+    }
+    if (more) {
+      turn_window(kb + TURN);
+      fetch_k(kb + TURN);
+    }
+    const bool masked = kb + BK - 1 > all_see || kb + BK > k1;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      float top = kRowLow;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (masked && kb + 4 * g + i > last[rt]) t[rt][i] = -INFINITY;
+        top = fmaxf(top, t[rt][i]);
+      }
+      top = groups_max(top);
+      const bool raise = top > m[rt] + kRowSlack;
+      if (__any(raise)) {
+        const float f = raise ? __builtin_amdgcn_exp2f(m[rt] - top) : 1.f;
+        if (raise) m[rt] = top;
+        l[rt] *= f;
+#pragma unroll
+        for (int x = 0; x < DX; ++x) o[rt][x] *= f;
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        t[rt][i] = __builtin_amdgcn_exp2f(t[rt][i] - m[rt]);
+        l[rt] += t[rt][i];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int x = 0; x < DX; ++x)
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) o[rt][x] = __builtin_amdgcn_mfma_f32_16x16x4f32(vv[i][x / 4][x % 4], t[rt][i], o[rt][x], 0, 0, 0);
+    if (more) fetch_v(kb + TURN);
+  }
+
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const float lt = groups_sum(l[rt]);
+    __syncthreads();
+    float* mo = sm_o + wave * 16 * OLD;
+#pragma unroll
+    for (int hh = 0; hh < VH; ++hh)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<f32x4*>(mo + l16 * OLD + 64 * hh + 16 * g + 4 * i) =
+            f32x4{o[rt][4 * hh][i], o[rt][4 * hh + 1][i], o[rt][4 * hh + 2][i], o[rt][4 * hh + 3][i]};
+    if (g == 0) {
+      sm_ml[wave][l16][0] = m[rt];
+      sm_ml[wave][l16][1] = lt;
+    }
+    __syncthreads();
+    merge_waves<float, D>(a, it, h, it.rc * R + 16 * rt, sm_o, sm_ml);
+  }
+}
+
+template <int D>
+hipError_t launch_rows(const ChunkArgs& a, int rows16, int items, int chunks, hipStream_t s) {
+  const dim3 grid(items, a.Hkv), block(kRowThreads);
+  if (rows16 == 1) hipLaunchKernelGGL((chunk_rows_f32_kernel<D, 1>), grid, block, 0, s, a);
+  else if (rows16 == 2) hipLaunchKernelGGL((chunk_rows_f32_kernel<D, 2>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((chunk_rows_f32_kernel<D, 4>), grid, block, 0, s, a);
+  if (a.p.max_splits > 1) hipLaunchKernelGGL((chunk_merge_kernel<float, D>), dim3(chunks, a.Hkv), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_chunk_f32(const ChunkArgs& a, int D, int rows16, int items, int chunks, hipStream_t s) {
+  return D == 128 ? launch_rows<128>(a, rows16, items, chunks, s) : launch_rows<64>(a, rows16, items, chunks, s);
+}
+
+}  // namespace seka
