@@ -12,7 +12,7 @@ LIB = os.path.join(HERE, "libseka.so")
 PROBES = ["mfma_rate_probe", "hbm_read_probe"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
-SOURCES = ["api.hip", "route.hip", "edit.hip", "decode.hip", "learn.hip", "rotary.hip", "chunk.hip", "chunk_f32.hip", "weights.hip", "evict.hip", "attn_f32.hip", "attn_bf16.hip", "attn_bf16_d128.hip", "attn_bf16_d64.hip",
+SOURCES = ["api.hip", "route.hip", "edit.hip", "decode.hip", "learn.hip", "rotary.hip", "chunk.hip", "chunk_f32.hip", "chunk_pipe_d128.hip", "chunk_pipe_d64.hip", "weights.hip", "evict.hip", "attn_f32.hip", "attn_bf16.hip", "attn_bf16_d128.hip", "attn_bf16_d64.hip",
            "attn_bf16_pipe_plain.hip", "attn_bf16_pipe_r32.hip", "attn_bf16_pipe_r64.hip", "attn_bf16_pipe_r128.hip",
            "attn_bf16_pipe64_plain.hip", "attn_bf16_pipe64_r32.hip", "attn_bf16_pipe64_r64.hip", "attn_bf16_pipe64_r128.hip"]
 

@@ -45,6 +45,7 @@
 #include <utility>
 
 #include "attn_bf16_lds_dma.h"
+#include "chunk_plan.h"
 
 namespace seka {
 
@@ -96,11 +97,11 @@ __device__ __forceinline__ void pipe_mfma_result_guard(f32x4 (&s)[2][2]) {
 }
 __device__ __forceinline__ void pipe_mfma_operand_guard(bf16x8 (&p)[2]) { asm volatile("s_nop 3" : "+v"(p[0]), "+v"(p[1])); }
 // What vector instructions made of the accumulators is complete here; the compiler may not move them past it.
-template <int N>
+template <int N, bool SUMS = true>
 __device__ __forceinline__ void pipe_pin_acc(f32x4 (&o)[N][2], f32x4 (&l)[2]) {
 #pragma unroll
   for (int i = 0; i < N; i += 2) asm volatile("" : "+v"(o[i][0]), "+v"(o[i][1]), "+v"(o[i + 1][0]), "+v"(o[i + 1][1]));
-  asm volatile("" : "+v"(l[0]), "+v"(l[1]));
+  if (SUMS) asm volatile("" : "+v"(l[0]), "+v"(l[1]));
 }
 
 __device__ __forceinline__ float pipe_max3(float a, float b, float c) {
@@ -204,11 +205,44 @@ constexpr int pipe_element_at(int m, int mfmas) {
   return -1;
 }
 
+struct PipeDense {};             // the arguments of pages where there are none
+
+// New tokens that see no key (more of them than cached tokens): the requests item, item + width, .. of a head chunk.
+template <int D, int HPW>
+__device__ __forceinline__ void pipe_rows_without_keys(const ChunkArgs& pg, int item, int hc) {
+  const int lane = threadIdx.x & 63;
+  for (int b0 = 0; b0 < pg.r.B; b0 += 64) {
+    ChunkExtent e = {0, 0, 0};
+    const int mine = b0 + lane;
+    if (mine < pg.r.B && mine % pg.width == item) e = chunk_extent(pg.r, pg.c, mine);
+    unsigned long long todo = __ballot(e.n > e.len);
+    for (; todo; todo &= todo - 1) {       // rare: lengths that do not count the new tokens
+      const int l = __builtin_ctzll(todo);
+      const int rows = __shfl(e.n - e.len, l), row0 = __shfl(e.row0, l);
+      for (int x = threadIdx.x; x < rows * HPW * (D / 8); x += blockDim.x) {
+        const size_t row = (size_t)(row0 + x / (HPW * (D / 8))) * pg.Hq + hc * HPW;
+        reinterpret_cast<uint4*>(static_cast<uint16_t*>(pg.O) + row * D)[x % (HPW * (D / 8))] = make_uint4(0, 0, 0, 0);
+      }
+      if (pg.lse)
+        for (int x = threadIdx.x; x < rows * HPW; x += blockDim.x) pg.lse[(size_t)(hc * HPW + x % HPW) * pg.r.total + row0 + x / HPW] = -INFINITY;
+    }
+  }
+}
+
+template <class PIECES, class PG>
+__device__ __forceinline__ PIECES pipe_pieces_of(const PG& pg, int item) {
+  if constexpr (std::is_same_v<PG, PipeDense>) return PIECES{};
+  else return PIECES(pg.r, pg.c, pg.width, item);
+}
+
 // HPW heads x RBW row groups = waves per workgroup; every wave owns 32 consecutive query rows, two row tiles of 16.
 // NKR: rank of the concatenated basis in blocks of 32 columns (compile-time so that the edit is straight-line code).
-template <int D, int HPW, int RBW, bool STEER, int NKR>
-__global__ __launch_bounds__(64 * HPW * RBW) __attribute__((amdgpu_waves_per_eu(2, D == 64 ? 2 : 8))) void
-attention_bf16_pipe_kernel(AttnArgs a, SteerArgs st) {
+// PAGED: keys and values in pages (seka_attention_chunk, pg); a workgroup's pieces come from chunk_plan.h.  A piece is worked on as if
+// its first key were key 0: positions of rows and the number of keys are relative to it.
+template <int D, int HPW, int RBW, bool STEER, int NKR, class PG>
+__device__ __forceinline__ void attention_bf16_pipe_body(const AttnArgs& a, const SteerArgs& st, const PG& pg) {
+  constexpr bool PAGED = !std::is_same_v<PG, PipeDense>;
+  static_assert(!(PAGED && STEER), "keys in pages are edited before they are stored");
   static_assert(D == 64 || D == 128, "head dimensions of the tile layouts");
   constexpr int NW = HPW * RBW;
   constexpr int NT = 64 * NW;
@@ -258,19 +292,44 @@ attention_bf16_pipe_kernel(AttnArgs a, SteerArgs st) {
   const int hq0 = hc * HPW;
   const int h = hq0 / G;
   int b, slot, W = a.width;
-  if (a.slots) {
-    if (!pipe_ragged_item<BQ, D>(a, item, b, slot, W)) return;
-  } else {
-    b = item / a.width;
-    slot = item % a.width;
-  }
   size_t tok0;                               // first token of this prompt in the tensors
   int S;                                     // this prompt's length: rows and keys beyond it do not exist
-  prompt_extent(a, b, tok0, S);
-  const int nblocks = (S + BQ - 1) / BQ;
-  if (!a.slots && (a.cu || a.lens)) W = (nblocks + 1) / 2;
-  if (slot >= W || slot >= nblocks) return;  // workgroup-uniform, before any barrier
-  int qb = nblocks - 1 - slot;
+  int nblocks, qb;
+  using Pieces = std::conditional_t<PAGED, PipePieces<BQ>, PipeDense>;
+  [[maybe_unused]] Pieces pieces = pipe_pieces_of<Pieces>(pg, item);
+  [[maybe_unused]] PipePiece piece = {};
+  [[maybe_unused]] int key0 = 0;             // the piece's first key
+  [[maybe_unused]] int first_row = 0;        // position of the block of rows, and of the request's first new token, relative to key0
+  [[maybe_unused]] int first_new = 0;
+  auto take_piece = [&]() __attribute__((always_inline)) {
+    if constexpr (PAGED) {
+      key0 = 64 * piece.t0;
+      S = piece.e.len - key0;
+      const int ctx = piece.e.len - piece.e.n;
+      first_row = PipePlan<BQ>::first_row(piece.e) + piece.k * BQ - key0;
+      first_new = max(ctx, 0) - key0;
+      tok0 = (size_t)((long long)piece.e.row0 - ctx + key0);       // row of the tensors of position 0
+      b = piece.b;
+    }
+  };
+  if constexpr (PAGED) {
+    slot = nblocks = qb = 0;
+    pipe_rows_without_keys<D, HPW>(pg, item, hc);
+    if (!pieces.next(piece)) return;         // workgroup-uniform, before any barrier
+    take_piece();
+  } else {
+    if (a.slots) {
+      if (!pipe_ragged_item<BQ, D>(a, item, b, slot, W)) return;
+    } else {
+      b = item / a.width;
+      slot = item % a.width;
+    }
+    prompt_extent(a, b, tok0, S);
+    nblocks = (S + BQ - 1) / BQ;
+    if (!a.slots && (a.cu || a.lens)) W = (nblocks + 1) / 2;
+    if (slot >= W || slot >= nblocks) return;  // workgroup-uniform, before any barrier
+    qb = nblocks - 1 - slot;
+  }
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -278,7 +337,7 @@ attention_bf16_pipe_kernel(AttnArgs a, SteerArgs st) {
   const int hq = hq0 + wave / RBW;
   // Waves w and w + 4 share a SIMD: their row blocks are chosen to end on different tiles or halves of a tile.
   const int rb = RBW == 1 ? 0 : RBW == 2 ? (wave ^ (wave >> 2)) & 1 : RBW == 4 ? (wave & 3) ^ (wave >> 2 ? 3 : 0) : wave < 4 ? wave : 11 - wave;
-  int qw = qb * BQ + WR * rb;    // first query row of this wave
+  int qw = PAGED ? first_row + WR * rb : qb * BQ + WR * rb;    // first query row of this wave
   int qi0 = qw + l16;                      // this lane's query row in row tile 0 (tile 1: + 16)
 
   const float gain = STEER ? st.gain[h] : 0.f;
@@ -286,7 +345,7 @@ attention_bf16_pipe_kernel(AttnArgs a, SteerArgs st) {
   const bool steer_on = STEER && gain != 0.f;
 
   int last_key = min(S, qb * BQ + BQ) - 1;
-  int ntiles = last_key / BK + 1;          // the first block is the later one: its tile count bounds the second's
+  int ntiles = PAGED ? piece.t1 - piece.t0 : last_key / BK + 1;          // the first block is the later one: its tile count bounds the second's
 
   // ---- tile loads: scalar tile base + per-lane offset fixed for the whole kernel ----
   // Slot s of a tile is LDS bytes [1024 s, 1024 s + 1024) = 4 rows (8 at D = 64); lane l lands at row l / CH of them,
@@ -317,10 +376,11 @@ attention_bf16_pipe_kernel(AttnArgs a, SteerArgs st) {
 #pragma unroll
   for (int n = 0; n < SPW; ++n) {
     const int row = slot_row(n);
-    koff[n] = row * rowbytes + 16u * ((lane & (CH - 1)) ^ pipe_k_swizzle<D>(row));
-    voff[n] = row * rowbytes + 16u * ((lane & (CH - 1)) ^ pipe_v_swizzle<D>(row));
+    const uint32_t off = (PAGED ? lane / CH : row) * rowbytes;
+    koff[n] = off + 16u * ((lane & (CH - 1)) ^ pipe_k_swizzle<D>(row));
+    voff[n] = off + 16u * ((lane & (CH - 1)) ^ pipe_v_swizzle<D>(row));
   }
-  const size_t head_off = (tok0 * a.Hkv + h) * D * 2;          // bytes to this (batch, KV head), token 0
+  const size_t head_off = PAGED ? (size_t)h * D * 2 : (tok0 * a.Hkv + h) * D * 2;          // bytes to this (batch, KV head), token 0
   const unsigned char* Kbytes = reinterpret_cast<const unsigned char*>(Kg) + head_off;
   const unsigned char* Vbytes = reinterpret_cast<const unsigned char*>(Vg) + head_off;
   // ring position (byte offset inside the V ring) of 32-key block j >= -1
@@ -328,8 +388,49 @@ attention_bf16_pipe_kernel(AttnArgs a, SteerArgs st) {
   // K tile t into its ring stage.  `full`: every row of the tile exists (no clamping, offsets fixed per lane).
   // Otherwise rows past the prompt's end repeat its last key (finite data that the causal mask hides); offsets
   // are then taken from token 0 so that they never go negative.
+  // PAGED: the rows of one load (64 / CH <= 8) lie in one page.  The numbers of the piece's pages wait in LDS; lane n of `pages` holds the one of
+  // load n of the K tile that is requested next, lane SPW + n that of the shifted V tile, read an iteration ahead.
+  [[maybe_unused]] int* const page_list = reinterpret_cast<int*>(smem + 2 * DMA_STAGES * TB + (D == 64 ? 4096 * NW : 0));
+  [[maybe_unused]] int pages = 0;
+  [[maybe_unused]] const int page_row = [&]() __attribute__((always_inline)) {      // of this lane's load in its tile
+    const int n = lane % SPW, v = lane / SPW;
+    return (64 / CH) * (SLOTS % NW == 0 ? wave + NW * n : min(wave + NW * n, SLOTS - 1)) - (v == 1 ? BK / 2 : 0);
+  }();
+  auto read_pages = [&](int t) __attribute__((always_inline)) {
+    const int key = min(max(t * BK + page_row, 0), min(S, ntiles * BK + BK) - 1);
+    if constexpr (PAGED) pages = page_list[((key + key0) >> pg.c.shift) - (key0 >> pg.c.shift)];
+  };
+  auto page_base = [&](const unsigned char* pool, int entry, int key) __attribute__((always_inline)) -> const unsigned char* {
+    if constexpr (PAGED) {
+      const uint32_t page = __builtin_amdgcn_readlane(pages, entry);
+      return pool + (((uint64_t)page << pg.c.shift) + (uint32_t)((key + key0) & ((1 << pg.c.shift) - 1))) * rowbytes;
+    }
+    return pool;
+  };
+  // page numbers of the piece, clamped into the pool
+  auto stage_pages = [&]() __attribute__((always_inline)) {
+    if constexpr (PAGED) {
+      const int p0 = key0 >> pg.c.shift, p1 = (min(S, ntiles * BK + BK) - 1 + key0) >> pg.c.shift;
+      for (int i = p0 + tid; i <= p1; i += NT) page_list[i - p0] = page_of(pg.c, b, i << pg.c.shift);
+      __syncthreads();
+    }
+  };
   auto issue_k_to = [&](auto full_c, int t, uint32_t lds_stage_base) __attribute__((always_inline)) {
     const int w = opaque_wave();
+    if constexpr (PAGED) {
+#pragma unroll
+      for (int n = 0; n < SPW; ++n) {
+        const int first = t * BK + (64 / CH) * slot_of(w, n);
+        if (decltype(full_c)::value || t * BK + BK <= S) {
+          pipe_load_16B(page_base(Kbytes, n, first), koff[n], lds_stage_base + slot_lds(w, n));
+        } else {                             // rows past the last key repeat it
+          const int row = min(first, S - 1);
+          pipe_load_16B(page_base(Kbytes, n, row), koff[n] + (uint32_t)(min(first + lane / CH, S - 1) - row - lane / CH) * rowbytes,
+                        lds_stage_base + slot_lds(w, n));
+        }
+      }
+      return;
+    }
     if (decltype(full_c)::value || t * BK + BK <= S) {
       // (a product of 32-bit factors: of 64-bit ones it took five scalar instructions more per tile)
       const unsigned char* tile = Kbytes + (uint64_t)(uint32_t)(t * BK) * rowbytes;
@@ -350,6 +451,20 @@ attention_bf16_pipe_kernel(AttnArgs a, SteerArgs st) {
   auto issue_v_to = [&](auto full_c, int t, uint32_t posA, uint32_t posB) __attribute__((always_inline)) {
     const int w = opaque_wave();
     const int first = t * BK - BK / 2;
+    if constexpr (PAGED) {
+#pragma unroll
+      for (int n = 0; n < SPW; ++n) {
+        const int key = first + (64 / CH) * slot_of(w, n);
+        const uint32_t lds = vst_base + (vslot_hi(w, n) ? posB : posA) + vslot_lds(w, n);
+        if (decltype(full_c)::value || (first >= 0 && first + BK <= S)) {
+          pipe_load_16B(page_base(Vbytes, SPW + n, key), voff[n], lds);
+        } else {
+          const int row = min(max(key, 0), S - 1);
+          pipe_load_16B(page_base(Vbytes, SPW + n, row), voff[n] + (uint32_t)(min(max(key + lane / CH, 0), S - 1) - row - lane / CH) * rowbytes, lds);
+        }
+      }
+      return;
+    }
     if (decltype(full_c)::value || (first >= 0 && first + BK <= S)) {
       const unsigned char* tile = Vbytes + (uint64_t)(uint32_t)first * rowbytes;
 #pragma unroll
@@ -394,17 +509,24 @@ attention_bf16_pipe_kernel(AttnArgs a, SteerArgs st) {
   // First loads of a block of query rows: K tiles 0 and 1, V blocks -1 (a copy of row 0: the first step's PV
   // product multiplies it by zero probabilities, so it only has to be finite) to 2, then the wave's Q rows.
   auto begin_block = [&]() __attribute__((always_inline)) {
+    if constexpr (PAGED) {
+      stage_pages();
+      read_pages(0);
+    }
     issue_k(0);
     issue_v(0);
+    if constexpr (PAGED) read_pages(1);
     if (ntiles > 1) issue_k(1);
     issue_v(1);
+    if constexpr (PAGED) read_pages(2);
     // Raw order: register i of lane l holds 16-byte chunk (l % 8) + 8 (i / 4) of row 8 (i % 4) + l / 8, so every load
     // covers eight whole 128-byte lines; q_operands() turns them into operands through LDS.  (Fetched in operand
     // order, 32 rows x 32 bytes per load, the address unit took 3 cycles per row: 6000 cycles per block.)
 #pragma unroll
     for (int i = 0; i < 2 * KS; ++i) {    // rows past the end read row 0 (finite data, results never stored):
       const int qi = qw + 8 * (i & 3) + (lane >> 3);                                          // no branch, no wait here
-      const uint16_t* qp = Qg + ((tok0 + (qi < S ? qi : 0)) * a.Hq + hq) * D + 64 * (i >> 2) + 8 * (lane & 7);
+      const bool there = qi < S && (!PAGED || qi >= first_new);
+      const uint16_t* qp = Qg + ((tok0 + (there ? qi : PAGED ? first_new : 0)) * a.Hq + hq) * D + 64 * (i >> 2) + 8 * (lane & 7);
       qf[i] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(qp));
     }
   };
@@ -775,7 +897,10 @@ attention_bf16_pipe_kernel(AttnArgs a, SteerArgs st) {
     for (int dt = 0; dt < DT; ++dt) oacc[dt][rt] = f32x4{0.f, 0.f, 0.f, 0.f};
     lacc[rt] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  pipe_pin_acc(oacc, lacc);
+  // PAGED: the row sums are those of the probabilities before their rounding (lse is then good to fp32), on the vector unit, this lane's
+  // keys only until the end
+  [[maybe_unused]] float l_run[2] = {0.f, 0.f};
+  pipe_pin_acc<DT, !PAGED>(oacc, lacc);
   const float c2 = a.scale * 1.4426950408889634f;   // probabilities are exp2(s * c2 - m)
   // m_run: reference exponent of the row (in units of s * c2).  It follows the row maximum lazily.  A row's first one is put kLead
   // above the maximum of its first block.  It is put there again where a probability of any row of the wave reaches 2, and
@@ -803,7 +928,7 @@ attention_bf16_pipe_kernel(AttnArgs a, SteerArgs st) {
   }
   const bf16x8 zeros8 = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
   bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
-  asm volatile("" : "+v"(ones));           // kept in registers
+  if (!PAGED) asm volatile("" : "+v"(ones));           // kept in registers
 
   // Scores of one 32-key block: S^T tiles [key tile][row tile]; off = LDS byte offset of the block's first row.
   auto kfrag = [&](int i, int off) __attribute__((always_inline)) -> bf16x8 {        // fragment i: slice i / 2, key tile i % 2
@@ -867,18 +992,23 @@ attention_bf16_pipe_kernel(AttnArgs a, SteerArgs st) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) oacc[dt][rt][i] *= alpha[rt];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) lacc[rt][i] *= alpha[rt];
+        for (int i = 0; i < (PAGED ? 0 : 4); ++i) lacc[rt][i] *= alpha[rt];
+        if (PAGED) l_run[rt] *= alpha[rt];
       }
-      pipe_pin_acc(oacc, lacc);
+      pipe_pin_acc<DT, !PAGED>(oacc, lacc);
     }
   };
   // Probabilities of one block, packed as P^T operands (lane group grp, slot e <-> key 16 (e / 4) + 4 grp + e % 4).
-  auto block_exp = [&](const f32x4 (&sv)[2][2], bf16x8 (&pb)[2]) __attribute__((always_inline)) {
+  auto block_exp = [&](const f32x4 (&sv)[2][2], bf16x8 (&pb)[2], float (&ls)[2]) __attribute__((always_inline)) {
 #pragma unroll
     for (int rt = 0; rt < 2; ++rt) {
       const float mneg = -m_run[rt];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) pb[rt][e] = (__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(sv[e >> 2][rt][e & 3], c2, mneg));
+      for (int e = 0; e < 8; ++e) {
+        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sv[e >> 2][rt][e & 3], c2, mneg));
+        pb[rt][e] = (__bf16)p;
+        if (PAGED) ls[rt] = e == 0 ? p : ls[rt] + p;
+      }
     }
   };
   // O^T += V^T P^T for one 32-key block, and the row sums of P^T (the rounded probabilities, those that the products use)
@@ -892,8 +1022,10 @@ attention_bf16_pipe_kernel(AttnArgs a, SteerArgs st) {
     }
     __builtin_amdgcn_sched_barrier(0);     // all of them on their way before the first product
     pipe_mfma_operand_guard(pb);
+    if (!PAGED) {
 #pragma unroll
-    for (int rt = 0; rt < 2; ++rt) pipe_mfma(lacc[rt], ones, pb[rt]);
+      for (int rt = 0; rt < 2; ++rt) pipe_mfma(lacc[rt], ones, pb[rt]);
+    }
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
       const bf16x4 lo4 = __builtin_bit_cast(bf16x4, lo[dt]), hi4 = __builtin_bit_cast(bf16x4, hi[dt]);
@@ -903,7 +1035,7 @@ attention_bf16_pipe_kernel(AttnArgs a, SteerArgs st) {
     }
   };
 
-  const bool wave_rows_exist = qw < S;
+  const bool wave_rows_exist = qw < S && (!PAGED || qw >= 0);      // PAGED: a piece may start behind the last key that a wave's rows see
   const int tw_last = wave_rows_exist ? min(ntiles - 1, (qw + WR - 1) / BK) : -1;   // last tile this wave computes on
 
   // ---- prologue: wait for the first tiles, edit K(0) and K(1), first block of S^T ----
@@ -1024,6 +1156,7 @@ attention_bf16_pipe_kernel(AttnArgs a, SteerArgs st) {
       if (t + 2 < ntiles) issue_k(t + 2);
       issue_v(t + 2);                                       // its first block belongs to tile t + 1
     }
+    if constexpr (PAGED) read_pages(t + 3);
   };
   auto bottom = [&](auto sure_c, int t) __attribute__((always_inline)) {
     if (decltype(sure_c)::value || t + 1 < ntiles) dma_wait_vmcnt<SPW>();   // all but the V loads of this iteration
@@ -1093,6 +1226,7 @@ attention_bf16_pipe_kernel(AttnArgs a, SteerArgs st) {
     bf16x8 kf[2 * KS];
     s16x4 vlo[DT], vhi[DT];
     float x[16], pr[16];
+    [[maybe_unused]] float ls[2] = {0.f, 0.f};
     bf16x2 pk[8];
     kf[0] = kpre[0];
     kf[1] = kpre[1];
@@ -1104,7 +1238,7 @@ attention_bf16_pipe_kernel(AttnArgs a, SteerArgs st) {
         if constexpr (f < 2) pipe_mfma_first(next[kt][rt], kf[f], qf[rt * KS + (f >> 1)]);
         else pipe_mfma(next[kt][rt], kf[f], qf[rt * KS + (f >> 1)]);
       } else if constexpr (m < NQ + 2) {
-        pipe_mfma(lacc[m - NQ], ones, pb[m - NQ]);
+        if constexpr (!PAGED) pipe_mfma(lacc[m - NQ], ones, pb[m - NQ]);
       } else {
         constexpr int dt = (m - NQ - 2) >> 1, rt = m & 1;
         const bf16x4 lo4 = __builtin_bit_cast(bf16x4, vlo[dt]), hi4 = __builtin_bit_cast(bf16x4, vhi[dt]);
@@ -1125,6 +1259,8 @@ attention_bf16_pipe_kernel(AttnArgs a, SteerArgs st) {
       // (volatile: the compiler would form all of them at the first one's place)
       if constexpr (e0 >= 0) asm volatile("v_fma_f32 %0, %1, %2, -%3" : "=v"(x[e0]) : "v"(cur[(e0 >> 2) & 1][e0 >> 3][e0 & 3]), "s"(c2), "v"(m_run[e0 >> 3]));
       if constexpr (e1 >= 0) pr[e1] = __builtin_amdgcn_exp2f(x[e1]);
+      // (as an addition in the language the sixteen would be summed behind the step, all of them kept until then)
+      if constexpr (PAGED && e2 >= 0) asm volatile("v_add_f32 %0, %0, %1" : "+v"(ls[e2 >> 3]) : "v"(pr[e2]));
       if constexpr (e2 >= 0 && (e2 & 1)) pk[e2 >> 1] = bf16x2{(__bf16)pr[e2 - 1], (__bf16)pr[e2]};
       __builtin_amdgcn_sched_barrier(0);
     });
@@ -1141,7 +1277,11 @@ attention_bf16_pipe_kernel(AttnArgs a, SteerArgs st) {
     if (__builtin_expect(__any((bits & 0x40004000u) != 0u), 0)) {
       // `cur` was produced by the previous step's MFMAs: far enough behind for the inline-assembly maxima
       raise_reference(cur);    // after this step's PV product, whose probabilities were formed against the old reference
-      block_exp(cur, pn);
+      block_exp(cur, pn, ls);
+    }
+    if (PAGED) {
+      l_run[0] += ls[0];
+      l_run[1] += ls[1];
     }
     pb[0] = pn[0];
     pb[1] = pn[1];
@@ -1213,7 +1353,8 @@ attention_bf16_pipe_kernel(AttnArgs a, SteerArgs st) {
       for (int dt = 0; dt < DT; ++dt) asm volatile("" : "+v"(vaddr[dt]));
 #pragma unroll
       for (int n = 0; n < SPW; ++n) asm volatile("" : "+v"(koff[n]), "+v"(voff[n]));
-      asm volatile("" : "+v"(ones), "+v"(m_run[0]), "+v"(m_run[1]));
+      if (!PAGED) asm volatile("" : "+v"(ones), "+v"(m_run[0]), "+v"(m_run[1]));
+      else asm volatile("" : "+v"(m_run[0]), "+v"(m_run[1]), "+v"(l_run[0]), "+v"(l_run[1]));
 #pragma nounroll
       for (; t + 3 <= t_hot && (!STEER || kEventsInHot || tile_evt > t + 3); t += 3) {
         hot(integral_constant<int, 0>{}, t);
@@ -1250,7 +1391,8 @@ attention_bf16_pipe_kernel(AttnArgs a, SteerArgs st) {
       // A wave whose rows are the first 32 of the tile sees nothing of its second block; one whose rows are the
       // last 32 sees all of its first.
       const int off = (t % 3) * TB;
-      const bool second = (qw & 32) != 0;      // wave-uniform
+      // (PAGED: or sees all of both, where its piece ends before its rows)
+      const bool second = PAGED ? qw >= t * BK + BK / 2 : (qw & 32) != 0;      // wave-uniform
       if (second) qk_block(off + HB, sc1);
       if (zt) {
         corr(std::false_type{}, t, 0, sc0);
@@ -1260,7 +1402,12 @@ attention_bf16_pipe_kernel(AttnArgs a, SteerArgs st) {
       auto last_block = [&](bool masked, bool empty, int j0, f32x4 (&sv)[2][2]) __attribute__((always_inline)) {
         if (masked) causal_mask(j0, sv);
         raise_reference(sv, empty);
-        block_exp(sv, pb);
+        float ls[2] = {0.f, 0.f};
+        block_exp(sv, pb, ls);
+        if (PAGED) {
+          l_run[0] += ls[0];
+          l_run[1] += ls[1];
+        }
       };
       last_block(!second, t == 0, t * BK, sc0);
       pv_block((int)vpos(2 * t), pb);
@@ -1279,23 +1426,49 @@ attention_bf16_pipe_kernel(AttnArgs a, SteerArgs st) {
   // ---- next block's first loads (after a barrier: the last PV product above still read the V ring), then this
   // block's output ----
   const int qw_out = qw;
-  const int dealt = (pass + 1) * W + (pass & 1 ? slot : W - 1 - slot);    // the next deal's block for this slot
-  const bool more = dealt < nblocks;
-  if (more) {
-    dma_barrier();
-    qb = nblocks - 1 - dealt;
-    qw = qb * BQ + WR * rb;
-    qi0 = qw + l16;
-    last_key = min(S, qb * BQ + BQ) - 1;
-    ntiles = last_key / BK + 1;
-    begin_block();
+  bool more;
+  if constexpr (PAGED) {
+    more = false;                          // the next piece's first loads follow the output (see the end of the loop)
+  } else {
+    const int dealt = (pass + 1) * W + (pass & 1 ? slot : W - 1 - slot);    // the next deal's block for this slot
+    more = dealt < nblocks;
+    if (more) {
+      dma_barrier();
+      qb = nblocks - 1 - dealt;
+      qw = qb * BQ + WR * rb;
+      qi0 = qw + l16;
+      last_key = min(S, qb * BQ + BQ) - 1;
+      ntiles = last_key / BK + 1;
+      begin_block();
+    }
   }
   if (!more) dma_barrier();    // the staging areas belong to the rings
   // Output: through the staging area, 64 of the 128 columns at a time, so that every store covers eight whole
   // 128-byte lines (straight from the accumulators a store is 32 pieces of 16 bytes: 13000 cycles per block).
   asm volatile("s_nop 15" ::: "memory");   // the last PV product
-  pipe_pin_acc(oacc, lacc);
+  pipe_pin_acc<DT, !PAGED>(oacc, lacc);
   const int ln = opaque_lane();
+  if constexpr (PAGED) {
+#pragma unroll
+    for (int rt = 0; rt < 2; ++rt) lacc[rt][0] = groups_sum(l_run[rt]);
+  }
+  bool joined = false;
+  if constexpr (PAGED) joined = !piece.whole;
+  if (joined) {
+    // a part of the block's keys: outputs as they are, reference exponent and sum, for the kernel that joins them
+    float* part = nullptr;
+    if constexpr (PAGED) part = pg.part + (((size_t)pieces.slot(piece) * nHC + hc) * (HPW * BQ) + (wave / RBW) * BQ + WR * rb) * (D + 4);
+#pragma unroll
+    for (int rt = 0; rt < 2; ++rt) {
+      float* const row = part + (16 * rt + (ln & 15)) * (D + 4);
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f32x4*>(row + 16 * dt + 4 * (ln >> 4)) = oacc[dt][rt];
+      if (ln < 16) {
+        row[D] = m_run[rt];
+        row[D + 1] = lacc[rt][0];
+      }
+    }
+  } else {
   const float inv[2] = {1.f / lacc[0][0], 1.f / lacc[1][0]};
 #pragma unroll
   for (int half = 0; half < D / 64; ++half) {
@@ -1313,17 +1486,37 @@ attention_bf16_pipe_kernel(AttnArgs a, SteerArgs st) {
     for (int i = 0; i < 4; ++i) {
       const int qi = qw_out + 8 * i + (ln >> 3);
       const u32x4 line = *stg_line(ln, i);
-      if (qi < S) *reinterpret_cast<u32x4*>(Og + ((tok0 + qi) * a.Hq + hq) * D + 64 * half + 8 * (ln & 7)) = line;
+      if (qi < S && (!PAGED || qi >= first_new)) *reinterpret_cast<u32x4*>(Og + ((tok0 + qi) * a.Hq + hq) * D + 64 * half + 8 * (ln & 7)) = line;
     }
     asm volatile("" ::: "memory");
   }
   // m_run is the reference exponent in units of s * scale * log2(e); the sums are relative to it
   if (a.lse && grp < 2) {                  // lane group rt writes row tile rt
     const int qi = qw_out + lane;
-    if (qi < S) a.lse[lse_index(a, b, hq, tok0, qi)] = (grp ? m_run[1] : m_run[0]) * 0.6931471805599453f + logf(grp ? lacc[1][0] : lacc[0][0]);
+    size_t at;
+    if constexpr (PAGED) at = (size_t)hq * pg.r.total + (tok0 + qi);
+    else at = lse_index(a, b, hq, tok0, qi);
+    if (qi < S && (!PAGED || qi >= first_new)) a.lse[at] = (grp ? m_run[1] : m_run[0]) * 0.6931471805599453f + logf(grp ? lacc[1][0] : lacc[0][0]);
   }
-  if (!more) break;
+  }   // whole
+  if constexpr (PAGED) {
+    if (!pieces.next(piece)) break;
+    dma_barrier();                         // the rings and the list of pages are free
+    take_piece();
+    qw = first_row + WR * rb;
+    qi0 = qw + l16;
+    ntiles = piece.t1 - piece.t0;
+    begin_block();
+  } else {
+    if (!more) break;
+  }
   }   // for pass
+}
+
+template <int D, int HPW, int RBW, bool STEER, int NKR>
+__global__ __launch_bounds__(64 * HPW * RBW) __attribute__((amdgpu_waves_per_eu(2, D == 64 ? 2 : 8))) void
+attention_bf16_pipe_kernel(AttnArgs a, SteerArgs st) {
+  attention_bf16_pipe_body<D, HPW, RBW, STEER, NKR>(a, st, PipeDense{});
 }
 
 }  // namespace seka

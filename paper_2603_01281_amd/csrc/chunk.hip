@@ -10,7 +10,9 @@
 // Keys and values are fetched as whole rows into registers, a block ahead, and pass through a wave-private LDS tile.
 #include <algorithm>
 
+#include "chunk_pipe.h"
 #include "chunk_rows.h"
+#include "compute_units.h"
 
 namespace seka {
 namespace {
@@ -230,18 +232,50 @@ RowPlan row_plan(int B, int S, int Hq, int Hkv, int dtype, int total, int max_q)
   return r;
 }
 
+int compute_units() {
+  static PerDeviceCount cus;
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess) return 256;
+  return cus.of(dev, [](int d) {
+    int n = 0;
+    return hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, d) == hipSuccess && n > 0 ? n : 256;
+  });
+}
+
+// Whether a call's chunks go to the pipelined kernel, and how: bf16, more rows per KV head than four tiles of 16, and a cache
+// whose page numbers fit beside the tiles in LDS (4 bytes for every page of S tokens).
+bool pipe_plan(int S, int Hq, int Hkv, int D, int dtype, int shift, int total, int max_q, PipeChunkPlan* out) {
+  const int G = Hq / Hkv;
+  if (dtype != SEKA_BF16 || (long long)std::min(max_q, total) * G <= 64) return false;
+  out->hpw = G % 4 == 0 ? 4 : G % 7 == 0 ? 7 : G % 2 == 0 ? 2 : 1;
+  out->rbw = out->hpw == 7 ? 1 : 8 / out->hpw;
+  const int nHC = Hq / out->hpw, cus = compute_units();
+  out->width = std::max(1, cus / nHC);
+  out->smem = attention_bf16_pipe_smem_bytes(D, 0, false, 1, out->hpw * out->rbw) + (((size_t)S >> shift) + 2) * sizeof(int);
+  out->workspace = out->width > 1 ? (size_t)2 * out->width * Hq * (32 * out->rbw) * (D + 4) * sizeof(float) : 0;
+  return out->smem <= 160 * 1024;
+}
+
 }  // namespace
 
 hipError_t launch_chunk_bf16(const ChunkArgs& a, int D, int rows16, int items, int chunks, hipStream_t s) {
   return D == 128 ? launch_rows<128>(a, rows16, items, chunks, s) : launch_rows<64>(a, rows16, items, chunks, s);
 }
 
+// (the larger need: which kernel runs depends on the page size too)
 size_t chunk_workspace_bytes(int B, int S, int Hq, int Hkv, int D, int dtype, int total, int max_q) {
   const RowPlan r = row_plan(B, S, Hq, Hkv, dtype, total, max_q);
-  return r.p.max_splits > 1 ? (size_t)r.items * Hkv * r.p.R * (D + 4) * sizeof(float) : 0;
+  const size_t rows = r.p.max_splits > 1 ? (size_t)r.items * Hkv * r.p.R * (D + 4) * sizeof(float) : 0;
+  PipeChunkPlan p;
+  return pipe_plan(S, Hq, Hkv, D, dtype, 16, total, max_q, &p) ? std::max(rows, p.workspace) : rows;
 }
 
 hipError_t launch_chunk(ChunkArgs a, int D, int dtype, int S, hipStream_t s) {
+  PipeChunkPlan p;
+  if (pipe_plan(S, a.Hq, a.Hkv, D, dtype, a.c.shift, a.r.total, a.r.max_q, &p)) {
+    a.width = p.width;
+    return D == 128 ? launch_chunk_pipe_d128(a, p, s) : launch_chunk_pipe_d64(a, p, s);
+  }
   const RowPlan r = row_plan(a.r.B, S, a.Hq, a.Hkv, dtype, a.r.total, a.r.max_q);
   a.p = r.p;
   a.items = r.items;

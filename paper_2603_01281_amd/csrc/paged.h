@@ -155,6 +155,7 @@ struct ChunkArgs {
   int items;              // (chunk, range) pairs that are launched and have room in part
   float* part;            // partial states: [item, Hkv, R, D + 4]: outputs, reference exponent (base 2), sum
   int Hq, Hkv;
+  int width;              // long chunks: workgroups per head chunk (chunk_plan.h)
   float scale;
 };
 

@@ -82,6 +82,19 @@ def test_long_cache_in_many_ranges(seka, dtype):
     check(seka, P.Pages(dtype, [1, 2, 20], [5000, 9, 3001], 8, 2, 128, 16, seed=10), f"ranges {dtype}")
 
 
+@pytest.mark.parametrize("Hq,Hkv,n,S", [(256, 64, 300, 900), (256, 64, 520, 1101), (256, 64, 256, 520), (1024, 64, 17, 150), (192, 64, 300, 700)])
+def test_long_chunk_of_many_heads(seka, Hq, Hkv, n, S):
+    """Few workgroups per head: a single request takes blocks of rows whole, and cuts the ones left over."""
+    check(seka, P.Pages("bf16", [n], [S], Hq, Hkv, 64, 16, seed=n), f"whole blocks {Hq}/{Hkv} {n} {S}")
+
+
+def test_blocks_cut_by_many_workgroups(seka):
+    """One head: every block of rows is cut into many pieces; requests of very different lengths share workgroups."""
+    check(seka, P.Pages("bf16", [33], [9000], 4, 1, 128, 16, seed=1), "pieces of one block")
+    check(seka, P.Pages("bf16", [100, 1, 0, 17, 1], [5000, 3, 700, 1200, 2000], 4, 1, 64, 32, seed=2), "pieces of mixed requests")
+    check(seka, P.Pages("bf16", [90, 300], [90, 2300], 7, 1, 128, 8, seed=3), "pieces, seven heads")
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_scores_that_grow(seka, dtype):
     """Every block of keys outgrows the reference of the one before: references are raised all along a row."""
