@@ -252,7 +252,8 @@ bool pipe_plan(int S, int Hq, int Hkv, int D, int dtype, int shift, int total, i
   const int nHC = Hq / out->hpw, cus = compute_units();
   out->width = std::max(1, cus / nHC);
   out->smem = attention_bf16_pipe_smem_bytes(D, 0, false, 1, out->hpw * out->rbw) + (((size_t)S >> shift) + 2) * sizeof(int);
-  out->workspace = out->width > 1 ? (size_t)2 * out->width * Hq * (32 * out->rbw) * (D + 4) * sizeof(float) : 0;
+  out->cuts = (size_t)2 * out->width * Hq * (32 * out->rbw) * (D + 4) * sizeof(float);      // behind the states, two per workgroup
+  out->workspace = out->cuts + (size_t)out->width * sizeof(int4);
   return out->smem <= 160 * 1024;
 }
 
@@ -274,6 +275,7 @@ hipError_t launch_chunk(ChunkArgs a, int D, int dtype, int S, hipStream_t s) {
   PipeChunkPlan p;
   if (pipe_plan(S, a.Hq, a.Hkv, D, dtype, a.c.shift, a.r.total, a.r.max_q, &p)) {
     a.width = p.width;
+    a.cuts = reinterpret_cast<int4*>(reinterpret_cast<char*>(a.part) + p.cuts);
     return D == 128 ? launch_chunk_pipe_d128(a, p, s) : launch_chunk_pipe_d64(a, p, s);
   }
   const RowPlan r = row_plan(a.r.B, S, a.Hq, a.Hkv, dtype, a.r.total, a.r.max_q);

@@ -15,57 +15,58 @@ __global__ __launch_bounds__(64 * HPW * RBW) __attribute__((amdgpu_waves_per_eu(
   attention_bf16_pipe_body<D, HPW, RBW, false, 1>(a, SteerArgs{}, pg);
 }
 
-// blockIdx: x: workgroup w whose piece starts inside a block, y: head chunk and 32 of its rows.  The block's states: the end of the piece before
-// w, then the starts of w's and of every later piece that starts in it too.
+// blockIdx: x: workgroup w whose piece starts inside a block, y: head chunk and some of its rows, four columns to a thread.  The block's
+// states: the end of the piece before w, then the starts of w's and of every later piece that starts in it too.
+constexpr int kJoinThreads = 256;
 template <int D, int HPW, int RBW>
-__global__ __launch_bounds__(256) void chunk_pipe_join_kernel(ChunkArgs pg) {
-  constexpr int BQ = 32 * RBW, PARTS = HPW * RBW;
+__global__ __launch_bounds__(kJoinThreads) void chunk_pipe_join_kernel(ChunkArgs pg) {
+  constexpr int BQ = 32 * RBW, ROWS = kJoinThreads / (D / 4), PARTS = HPW * BQ / ROWS;
   const int w = blockIdx.x + 1, hc = blockIdx.y / PARTS, part = blockIdx.y % PARTS, nHC = pg.Hq / HPW;
-  const PipePlan<BQ> plan(pg.r, pg.c, pg.width);
-  if (w >= plan.W) return;
-  const PipeCut here = plan.cut(w);
-  if (here.t == 0 || here.b >= pg.r.B) return;
-  const PipeCut prev = plan.cut(w - 1);
-  if (prev.b == here.b && prev.k == here.k && prev.t > 0) return;      // an earlier workgroup's
-  int pieces = 2;
-  for (int v = w + 1; v < plan.W; ++v) {
-    const PipeCut later = plan.cut(v);
-    if (later.b != here.b || later.k != here.k || later.t == 0) break;
-    ++pieces;
+  const int4 here = pg.cuts[w], prev = pg.cuts[w - 1];
+  if (here.z == 0 || here.x >= pg.r.B) return;
+  if (prev.x == here.x && prev.y == here.y && prev.z > 0) return;      // an earlier workgroup's
+  int pieces = 1;
+  for (int v = w; v < pg.width; v += 64) {                             // this one and those behind it that start in the same block
+    const int mine = v + (threadIdx.x & 63);
+    int4 x = make_int4(-1, 0, 0, 0);
+    if (mine < pg.width) x = pg.cuts[mine];
+    const unsigned long long other = ~__ballot(x.x == here.x && x.y == here.y && x.z > 0);
+    pieces += other ? __builtin_ctzll(other) : 64;
+    if (other) break;
   }
-  const ChunkExtent e = plan.extent(here.b);
-  const int ctx = e.len - e.n, hq = hc * HPW + part / RBW;
-  const int pos0 = PipePlan<BQ>::first_row(e) + here.k * BQ + 32 * (part % RBW);
+  const ChunkExtent e = chunk_extent(pg.r, pg.c, here.x);
+  const int r = part * ROWS + threadIdx.x / (D / 4), d = threadIdx.x % (D / 4) * 4;      // row of the workgroup: head, position
+  const int ctx = e.len - e.n, hq = hc * HPW + r / BQ;
+  const int pos = PipePlan<BQ>::first_row(e) + here.y * BQ + r % BQ, i = pos - ctx;
+  if (pos < max(ctx, 0) || i >= e.n) return;
   const size_t stride = (size_t)2 * nHC * (HPW * BQ) * (D + 4);        // from a slot of one workgroup to the next one's
-  const float* base = pg.part + ((size_t)(2 * w) * nHC + hc) * (HPW * BQ) * (D + 4) + (size_t)part * 32 * (D + 4);
-  for (int idx = threadIdx.x; idx < 32 * (D / 4); idx += 256) {
-    const int r = idx / (D / 4), d = idx % (D / 4) * 4, i = pos0 + r - ctx;
-    if (pos0 + r < max(ctx, 0) || i >= e.n) continue;
-    const float* ps = base + (size_t)r * (D + 4) - stride / 2;         // slot 2 w - 1
-    float m = -1e30f, l = 0.f;
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < pieces; ++s) {
-      const float m2 = ps[D], l2 = ps[D + 1];
-      const f32x4 o2 = *reinterpret_cast<const f32x4*>(ps + d);
-      const float mm = fmaxf(m, m2), f1 = __builtin_amdgcn_exp2f(m - mm), f2 = __builtin_amdgcn_exp2f(m2 - mm);
-      m = mm;
-      l = l * f1 + l2 * f2;
-      o = o * f1 + o2 * f2;
-      ps += s == 0 ? stride / 2 : stride;
-    }
-    const float inv = 1.f / l;
-    bf16x4 v;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] = (__bf16)(o[k] * inv);
-    *reinterpret_cast<bf16x4*>(static_cast<uint16_t*>(pg.O) + ((size_t)(e.row0 + i) * pg.Hq + hq) * D + d) = v;
-    if (pg.lse && d == 0) pg.lse[(size_t)hq * pg.r.total + e.row0 + i] = m * 0.6931471805599453f + logf(l);
+  const float* first = pg.part + ((size_t)(2 * w) * nHC + hc) * (HPW * BQ) * (D + 4) + (size_t)r * (D + 4);       // slot 2 w; the end before it: 2 w - 1
+  const float* before = first - stride / 2;
+  float m = before[D];
+#pragma unroll 4
+  for (int s = 0; s < pieces - 1; ++s) m = fmaxf(m, first[s * stride + D]);
+  const float f0 = __builtin_amdgcn_exp2f(before[D] - m);
+  float l = before[D + 1] * f0;
+  f32x4 o = *reinterpret_cast<const f32x4*>(before + d) * f0;
+#pragma unroll 4
+  for (int s = 0; s < pieces - 1; ++s) {
+    const float* ps = first + s * stride;
+    const float f = __builtin_amdgcn_exp2f(ps[D] - m);
+    l += ps[D + 1] * f;
+    o += *reinterpret_cast<const f32x4*>(ps + d) * f;
   }
+  const float inv = 1.f / l;
+  bf16x4 v;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) v[k] = (__bf16)(o[k] * inv);
+  *reinterpret_cast<bf16x4*>(static_cast<uint16_t*>(pg.O) + ((size_t)(e.row0 + i) * pg.Hq + hq) * D + d) = v;
+  if (pg.lse && d == 0) pg.lse[(size_t)hq * pg.r.total + e.row0 + i] = m * 0.6931471805599453f + logf(l);
 }
 
 struct PipeChunkPlan {
   int hpw, rbw;          // heads and blocks of 32 rows of a workgroup
   int width;             // workgroups per head chunk
-  size_t smem, workspace;
+  size_t smem, cuts, workspace;          // cuts: their offset in the workspace
 };
 
 hipError_t launch_chunk_pipe_d128(const ChunkArgs& a, const PipeChunkPlan& p, hipStream_t s);
@@ -78,7 +79,7 @@ hipError_t launch_chunk_pipe_cfg(const ChunkArgs& a, const PipeChunkPlan& p, hip
   if (e != hipSuccess) return e;
   const int nHC = a.Hq / HPW;
   hipLaunchKernelGGL(kernel, dim3((unsigned)(p.width * nHC)), dim3(64 * HPW * RBW), p.smem, s, a);
-  if (p.width > 1) hipLaunchKernelGGL((chunk_pipe_join_kernel<D, HPW, RBW>), dim3(p.width - 1, nHC * HPW * RBW), dim3(256), 0, s, a);
+  if (p.width > 1) hipLaunchKernelGGL((chunk_pipe_join_kernel<D, HPW, RBW>), dim3(p.width - 1, a.Hq * (32 * RBW) / (kJoinThreads / (D / 4))), dim3(kJoinThreads), 0, s, a);
   return hipGetLastError();
 }
 

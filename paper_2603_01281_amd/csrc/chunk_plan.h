@@ -8,7 +8,7 @@
 // piece starts and ends anywhere in a block, at a tile, and the states of a block that was cut are joined by a second kernel.  A
 // single long request (the chunk no longer than what precedes it) takes whole blocks in step, so that the workgroups of an XCD read the same tiles
 // at the same time, and only what is left over by them is cut.
-// Every workgroup, and the joining kernel, finds its pieces from the lengths by itself, in integers.
+// Every workgroup finds its pieces from the lengths by itself, and leaves where the first one starts for the joining kernel.
 #pragma once
 #include "paged.h"
 
@@ -27,23 +27,25 @@ struct PipePlan {
   static constexpr long long s = BQ / 32;
   ChunkRows r;
   PagedCache c;
+  ChunkExtent mine;      // request `lane`, where there are no more than 64
+  long long ends;        // and the half tiles of the requests up to it
   long long T, per;      // half tiles of all blocks; of a workgroup
   int W;                 // workgroups that get work
   int rem, rounds;       // a single long request: blocks that are cut, whole blocks per workgroup; rounds = 0: everything is cut
 
-  __device__ __forceinline__ PipePlan(const ChunkRows& rows, const PagedCache& cache, int width) : r(rows), c(cache) {
+  __device__ __forceinline__ PipePlan(const ChunkRows& rows, const PagedCache& cache, int width) : r(rows), c(cache), mine{0, 0, 0}, ends(0) {
     T = 0;
     const int lane = threadIdx.x & 63;
     for (int b0 = 0; b0 < r.B; b0 += 64) {
-      long long w = b0 + lane < r.B ? work_of(b0 + lane) : 0;
-#pragma unroll
-      for (int d = 1; d < 64; d <<= 1) w += __shfl_xor(w, d);
-      T += w;
+      ChunkExtent e = {0, 0, 0};
+      if (b0 + lane < r.B) e = chunk_extent(r, c, b0 + lane);
+      mine = e;
+      ends = sums(work(e));
+      T += uniform(__shfl(ends, 63));
     }
-    T = uniform(T);
     const long long fill = T >> kPipeLeastLog2;
     W = (int)(fill < 1 ? 1 : fill < width ? fill : width);
-    per = (T + W - 1) / W;
+    per = T < 0x80000000ll ? (long long)(((uint32_t)T + (uint32_t)W - 1) / (uint32_t)W) : (T + W - 1) / W;
     rem = rounds = 0;
     if (r.B == 1) {
       const ChunkExtent e = extent(0);
@@ -60,11 +62,27 @@ struct PipePlan {
     const uint32_t lo = __builtin_amdgcn_readfirstlane((int)(uint32_t)v), hi = __builtin_amdgcn_readfirstlane((int)(uint32_t)((unsigned long long)v >> 32));
     return (long long)((unsigned long long)hi << 32 | lo);
   }
+  __device__ __forceinline__ static long long sums(long long v) {      // inclusive, over the wave's lanes
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const long long o = __shfl_up(v, d);
+      if (lane >= d) v += o;
+    }
+    return v;
+  }
   __device__ __forceinline__ ChunkExtent extent(int b) const {
-    ChunkExtent e = chunk_extent(r, c, b);
-    e.row0 = uniform(e.row0);
-    e.n = uniform(e.n);
-    e.len = uniform(e.len);
+    ChunkExtent e;
+    if (r.B <= 64) {
+      e.row0 = __builtin_amdgcn_readlane(mine.row0, b);
+      e.n = __builtin_amdgcn_readlane(mine.n, b);
+      e.len = __builtin_amdgcn_readlane(mine.len, b);
+    } else {
+      e = chunk_extent(r, c, b);
+      e.row0 = uniform(e.row0);
+      e.n = uniform(e.n);
+      e.len = uniform(e.len);
+    }
     return e;
   }
   // position of the first block's first row
@@ -75,17 +93,14 @@ struct PipePlan {
   __device__ __forceinline__ static long long before(const ChunkExtent& e, long long k) {
     return k * (first_row(e) / 32 + kPipeOver) + s * (k * (k + 1) / 2);
   }
-  __device__ __forceinline__ long long work_of(int b) const {
-    const ChunkExtent e = chunk_extent(r, c, b);
-    return before(e, blocks(e));
-  }
+  __device__ __forceinline__ static long long work(const ChunkExtent& e) { return before(e, blocks(e)); }
 
   // block k's index of round i for workgroup w: back and forth
   __device__ __forceinline__ int whole(int w, int i) const { return rem + i * W + (i & 1 ? W - 1 - w : w); }
 
   // Where workgroup w's piece of the axis starts (w = W: where the axis ends).
   __device__ __forceinline__ PipeCut cut(int w) const {
-    long long x;
+    long long x = per * w;
     if (rounds > 0) {
       // the whole blocks of the workgroups before w are theirs already
       const ChunkExtent e = extent(0);
@@ -95,42 +110,45 @@ struct PipePlan {
         theirs += before(e, first + w) - before(e, first);
       }
       const long long all = before(e, rem);
-      x = w == W ? all : per * w - theirs;
+      x = w == W ? all : x - theirs;
       x = x < 0 ? 0 : x > all ? all : x;
       return at(e, 0, rem, x);
     }
-    x = per * w;
     if (x >= T) return PipeCut{r.B, 0, 0};
     const int lane = threadIdx.x & 63;
     long long passed = 0;
     for (int b0 = 0; b0 < r.B; b0 += 64) {
-      const long long mine = b0 + lane < r.B ? work_of(b0 + lane) : 0;
-      long long ends = mine;
-#pragma unroll
-      for (int d = 1; d < 64; d <<= 1) {
-        const long long o = __shfl_up(ends, d);
-        if (lane >= d) ends += o;
+      const bool held = r.B <= 64;
+      ChunkExtent e = mine;
+      if (!held) {
+        e = ChunkExtent{0, 0, 0};
+        if (b0 + lane < r.B) e = chunk_extent(r, c, b0 + lane);
       }
-      const unsigned long long hit = __ballot(x - passed < ends);
+      const long long own = work(e), upto = held ? ends : sums(own);
+      const unsigned long long hit = __ballot(x - passed < upto);
       if (hit != 0ull) {
         const int l = __builtin_ctzll(hit);
-        const long long start = passed + uniform(__shfl(ends - mine, l));
-        const ChunkExtent e = extent(b0 + l);
-        return at(e, b0 + l, blocks(e), x - start);
+        const long long start = passed + uniform(__shfl(upto - own, l));
+        const ChunkExtent eb = extent(b0 + l);
+        return at(eb, b0 + l, blocks(eb), x - start);
       }
-      passed += uniform(__shfl(ends, 63));
+      passed += uniform(__shfl(upto, 63));
     }
     return PipeCut{r.B, 0, 0};
   }
 
   // The place x half tiles into the first nb blocks of a request.
   __device__ __forceinline__ static PipeCut at(const ChunkExtent& e, int b, int nb, long long x) {
-    int k = 0;                           // the last block that starts at x or before
-    for (int bit = 1 << 26; bit; bit >>= 1)
-      if (k + bit <= nb && before(e, k + bit) <= x) k += bit;
+    // the last block that starts at x or before: s k (k + 1) / 2 + k f = x, put right by whole blocks (fp32: off by a few of millions)
+    const float f = (float)(first_row(e) / 32 + kPipeOver) + 0.5f * s;
+    const float root = 2.f * (float)x / (f + sqrtf(f * f + 2.f * s * (float)x));
+    int k = min(max((int)root, 0), nb);
+    while (k > 0 && before(e, k) > x) --k;
+    while (k < nb && before(e, k + 1) <= x) ++k;
+    k = uniform(k);
     if (k >= nb) return PipeCut{b, nb, 0};
     const long long into = x - before(e, k) - kPipeOver;
-    const int n = tiles(e, k), t = (int)(into < 0 ? 0 : into / 2);
+    const int n = tiles(e, k), t = uniform((int)(into < 0 ? 0 : into / 2));
     if (t < kPipeSnap) return PipeCut{b, k, 0};
     if (n - t < kPipeSnap) return PipeCut{b, k + 1, 0};
     return PipeCut{b, k, t};
@@ -149,16 +167,16 @@ template <int BQ>
 struct PipePieces {
   PipePlan<BQ> p;
   int w, round;
-  PipeCut now, end;
+  PipeCut now, end, start;
 
   __device__ __forceinline__ PipePieces(const ChunkRows& rows, const PagedCache& cache, int width, int workgroup)
       : p(rows, cache, width), w(workgroup), round(0) {
-    now = end = PipeCut{p.r.B, 0, 0};
+    now = end = start = PipeCut{p.r.B, 0, 0};
     if (w >= p.W) {
       round = p.rounds;
       return;
     }
-    now = p.cut(w);
+    start = now = p.cut(w);
     end = p.cut(w + 1);
   }
   __device__ __forceinline__ bool next(PipePiece& out) {

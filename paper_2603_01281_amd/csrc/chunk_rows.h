@@ -4,27 +4,9 @@
 
 namespace seka {
 
-constexpr int kRowWaves = 4, kRowThreads = 64 * kRowWaves;
+constexpr int kRowThreads = 64 * kRowWaves;
 constexpr float kRowSlack = 8.f;         // a row's reference exponent trails its maximum by at most this (base 2)
 constexpr float kRowLow = -1e30f;        // reference of a row that has seen nothing
-
-// Pages of a wave's next blocks of keys, one per lane: block n of the window is tokens k + 32 kRowWaves n .. + 31 (KEYS = 32).  A page
-// that is shorter than a block takes several lanes.
-template <int KEYS>
-struct PageWindow {
-  int entry;             // this lane's page
-  int per_block;         // lanes per block
-  int left;              // blocks of the window that are still to come
-
-  __device__ __forceinline__ void load(const PagedCache& c, int b, int key, int k1) {
-    const int lane = threadIdx.x & 63;
-    const int shift = min(c.shift, __builtin_ctz(KEYS));
-    per_block = KEYS >> shift;
-    left = 64 / per_block;
-    const int j = key + (lane / per_block) * KEYS * kRowWaves + ((lane % per_block) << shift);
-    entry = page_of(c, b, min(j, k1 - 1));
-  }
-};
 
 // Merged state of output column d of a row: the output itself if the item has its rows to itself, else a partial state.
 template <typename T, int D>

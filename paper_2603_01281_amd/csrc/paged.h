@@ -46,7 +46,7 @@ __device__ __forceinline__ int page_of(const PagedCache& c, int b, int j) {
 // of a call sees the same plan.  T = sum over chunks of their keys (in blocks of 32); a range has about T / slots blocks
 // and no fewer than least; slots is a power of two.
 struct ChunkPlan {
-  int R, G;               // rows per chunk, query heads per KV head
+  int R, G;               // rows per chunk, query heads per KV head; R = 0: one chunk for every request that has cached tokens
   int slots_log2;         // about so many ranges in all, per KV head
   int least;              // blocks of 32 keys in a range, at least
   int max_splits;
@@ -78,7 +78,7 @@ __device__ __forceinline__ bool plan_item(const ChunkRows& r, const PagedCache& 
     e = ChunkExtent{0, 0, 0};
     if (b0 + lane < r.B) {
       e = chunk_extent(r, c, b0 + lane);
-      chunks = (int)(((unsigned)e.n * (unsigned)p.G + p.R - 1) / (unsigned)p.R);
+      chunks = p.R ? (int)(((unsigned)e.n * (unsigned)p.G + p.R - 1) / (unsigned)p.R) : e.len > 0;
       blocks = (e.len + 31) >> 5;
     }
   };
@@ -124,7 +124,7 @@ __device__ __forceinline__ bool plan_item(const ChunkRows& r, const PagedCache& 
 // Keys that the last row of chunk rc sees, and the range of them that the item takes: whole blocks of 32 but for the last.
 __device__ __forceinline__ void plan_range(const ChunkPlan& p, const ChunkItem& it, int& k0, int& k1) {
   const int last_row = min((it.rc + 1) * p.R, it.e.n * p.G) - 1;
-  const int seen = min(max(it.e.len - it.e.n + last_row / p.G + 1, 0), it.e.len);
+  const int seen = p.R ? min(max(it.e.len - it.e.n + last_row / p.G + 1, 0), it.e.len) : it.e.len;
   const int per = (((seen + 31) >> 5) + it.splits - 1) / it.splits * 32;
   k0 = min(it.split * per, seen);
   k1 = min(k0 + per, seen);
@@ -145,6 +145,26 @@ __device__ __forceinline__ float groups_sum(float v) {
   return over_groups(v, [](float x, float y) __attribute__((always_inline)) { return x + y; });
 }
 
+constexpr int kRowWaves = 4;             // waves of a workgroup that take a range's blocks of keys in turn
+
+// Pages of a wave's next blocks of keys, one per lane: block n of the window is tokens k + 32 kRowWaves n .. + 31 (KEYS = 32).  A page
+// that is shorter than a block takes several lanes.
+template <int KEYS>
+struct PageWindow {
+  int entry;             // this lane's page
+  int per_block;         // lanes per block
+  int left;              // blocks of the window that are still to come
+
+  __device__ __forceinline__ void load(const PagedCache& c, int b, int key, int k1) {
+    const int lane = threadIdx.x & 63;
+    const int shift = min(c.shift, __builtin_ctz(KEYS));
+    per_block = KEYS >> shift;
+    left = 64 / per_block;
+    const int j = key + (lane / per_block) * KEYS * kRowWaves + ((lane % per_block) << shift);
+    entry = page_of(c, b, min(j, k1 - 1));
+  }
+};
+
 struct ChunkArgs {
   const void* Q;
   void* O;
@@ -156,6 +176,7 @@ struct ChunkArgs {
   float* part;            // partial states: [item, Hkv, R, D + 4]: outputs, reference exponent (base 2), sum
   int Hq, Hkv;
   int width;              // long chunks: workgroups per head chunk (chunk_plan.h)
+  int4* cuts;             // and where each of them starts: request, block, tile
   float scale;
 };
 
@@ -182,6 +203,7 @@ struct WeightsArgs {
   const float* W_in;      // dev [num_pages, Hkv, page_size] or nullptr
   PagedCache c;
   ChunkRows r;
+  ChunkPlan p;            // few rows: the ranges of the keys
   int Hq, Hkv, window;
   float scale, decay;
 };

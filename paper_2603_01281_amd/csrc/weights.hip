@@ -3,11 +3,16 @@
 //   W_out[b, h, j] = decay W_in[b, h, j] + sum over heads g of the group and the last `window` new tokens i that see j
 //                    of exp(scale q_{i,g} . k_j - lse_{i,g})
 //
-// A wave holds 16 KT keys in registers and passes the rows by (new token i and head g are row i G + g), 16 at a time:
-// S (rows x keys) = Q K^T, so that a lane has one key and four rows of every product, adds up its exponentials in place, and the
-// sums cross lanes once, behind the last row.  No scores, no atomics: the result does not depend on scheduling.
-// SHARE: the waves of a workgroup take the same keys and every fourth tile of rows, and join their sums in LDS; otherwise each
-// wave has keys of its own.
+// Rows: new token i and head g are row i G + g.  S (rows x keys) = Q K^T in tiles of 16 x 16: a lane has one key and four rows of
+// every product, adds up its exponentials in place, and the sums cross lanes once, behind the last row.  No scores in
+// memory, no atomics: the result does not depend on scheduling.
+//
+// Few rows (generation): HBM-bound, every key is read once.  weights_stream_kernel holds the rows and streams the keys as whole rows
+// through a wave-private LDS tile, a block ahead, over ranges that are cut as for the attention itself (paged.h, plan_item).
+// Many rows: bound by the vector unit (an exponential takes it four times as long as a multiplication; 96 cycles per tile of 16 x 16
+// against 64 of the matrix pipe at D = 128).  weights_block_kernel holds 64 keys per wave in registers and passes the rows by, 64 at a
+// time through LDS for all its waves.  weights_share_kernel, where those would leave compute units idle: 64 keys per workgroup,
+// every wave its share of the rows, straight from the caches; the waves' sums are joined in LDS.
 #include <algorithm>
 
 #include "paged.h"
@@ -15,7 +20,11 @@
 namespace seka {
 namespace {
 
-constexpr int kWtWaves = 4, kWtTiles = 4;       // waves, tiles of 16 keys per wave
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+constexpr int kWtWaves = 4, kWtThreads = 64 * kWtWaves;
+// tiles of 16 keys that a wave holds (four of fp32 rows of 512 bytes did not fit its registers)
+template <typename T, int D> constexpr int wt_tiles() { return D * sizeof(T) > 256 ? 2 : 4; }
+constexpr int kWtRows = 64;                     // rows that pass through LDS at a time
 
 template <typename T> struct WtMath;
 template <> struct WtMath<uint16_t> {
@@ -34,23 +43,156 @@ template <> struct WtMath<float> {
   }
 };
 
-template <typename T, int D, bool SHARE>
-__global__ __launch_bounds__(64 * kWtWaves, 2) void weights_kernel(WeightsArgs a) {
+// Scores of a tile: rows 4 grp + x of the lane's key.
+template <typename T, int NF>
+__device__ __forceinline__ f32x4 wt_tile(const typename WtMath<T>::frag (&q)[NF], const typename WtMath<T>::frag (&k)[NF]) {
   using M = WtMath<T>;
-  typedef typename M::frag frag;
-  constexpr int NF = D * sizeof(T) / 64, KT = kWtTiles, KEYS = 16 * KT;      // fragments of a row: 64 bytes over four lanes each
-  typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
-  __shared__ float sm[SHARE ? kWtWaves : 1][SHARE ? KEYS : 1];
+  f32x4 acc[M::CH];
+#pragma unroll
+  for (int c = 0; c < M::CH; ++c) acc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int f = 0; f < NF; ++f) M::mma(acc, q[f], k[f]);
+#pragma unroll
+  for (int half = M::CH / 2; half; half /= 2)
+#pragma unroll
+    for (int c = 0; c < half; ++c) acc[c] += acc[c + half];
+  return acc[0];
+}
 
-  const int b = blockIdx.z, h = blockIdx.y, G = a.Hq / a.Hkv;
+// A row's log-sum-exp in units of the exponent; rows that saw nothing count nothing: exp(. - inf) = 0.
+__device__ __forceinline__ float wt_reference(float lse) { return lse == -INFINITY ? INFINITY : lse * 1.4426950408889634f; }
+
+// ---- few rows ------------------------------------------------------------------------------------------------------------
+
+template <typename T, int D, int RT>
+__global__ __launch_bounds__(kRowWaves * 64, 2) void weights_stream_kernel(WeightsArgs a) {
+  typedef typename WtMath<T>::frag frag;
+  constexpr int RB = D * sizeof(T), NF = RB / 64;                       // bytes of a row, fragments of it: 64 bytes over four lanes each
+  constexpr int BK = sizeof(T) == 2 ? 32 : 16, KT = BK / 16;
+  constexpr int CPR = RB / 16, RPI = 64 / CPR, NV = BK / RPI;           // 16-byte pieces per row, rows per load, loads per block
+  constexpr int LD = RB + 16;                                           // LDS row stride (bytes): 16 rows at one piece, spread over all banks
+  __shared__ __attribute__((aligned(16))) unsigned char smem[kRowWaves * BK * LD];
+
+  ChunkItem it;
+  if (!plan_item<false>(a.r, a.c, a.p, blockIdx.x, it)) return;
+  int k0, k1;
+  plan_range(a.p, it, k0, k1);
+  const int h = blockIdx.y, G = a.Hq / a.Hkv;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, grp = lane >> 4;
-  const ChunkExtent e = chunk_extent(a.r, a.c, b);
-  const int kbase = SHARE ? blockIdx.x * KEYS : (blockIdx.x * kWtWaves + wave) * KEYS;
-  if (kbase >= e.len) return;              // SHARE: the whole workgroup; otherwise no barrier follows
+  const int ctx = it.e.len - it.e.n;
+  const int row_lo = max(it.e.n - a.window, 0) * G, rows = it.e.n * G;
+  unsigned char* tile = smem + wave * BK * LD;
 
-  // ---- keys: lane (key 16 kt + l16, bytes 64 f + 16 grp); behind the last one it is repeated ----
-  frag kf[KT][NF];
-  size_t home[KT];                         // of this lane's keys in the weights
+  frag q[RT][NF];
+  float ref[RT][4];
+  int last[RT][4];                         // last key that the row sees
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const int row = row_lo + 16 * rt + l16;
+    const bool ok = row < rows;
+    const int i = ok ? row / G : 0, hq = h * G + (ok ? row % G : 0);
+    const char* qp = static_cast<const char*>(a.Q) + ((size_t)(it.e.row0 + i) * a.Hq + hq) * RB + 16 * grp;
+#pragma unroll
+    for (int f = 0; f < NF; ++f) {
+      u32x4 v = {0, 0, 0, 0};
+      if (ok) v = *reinterpret_cast<const u32x4*>(qp + 64 * f);
+      q[rt][f] = __builtin_bit_cast(frag, v);
+    }
+    float r = INFINITY;
+    if (ok) r = wt_reference(a.lse[(size_t)hq * a.r.total + it.e.row0 + i]);
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      ref[rt][x] = __shfl(r, 4 * grp + x);
+      last[rt][x] = ctx + __shfl(i, 4 * grp + x);
+    }
+  }
+  const int all_see = ctx + row_lo / G;    // keys up to here are seen by every row
+  const float c2 = a.scale * 1.4426950408889634f;
+
+  const uint32_t row_bytes = (uint32_t)a.Hkv * RB;
+  const uint32_t lane_off = (uint32_t)(lane / CPR) * row_bytes + 16u * (lane % CPR);
+  const char* Kh = static_cast<const char*>(a.c.K) + (size_t)h * RB;
+  const int slots = (1 << a.c.shift) - 1;
+  u32x4 kr[NV];
+  float w_in = 0.f;
+  size_t home = 0, home_next = 0;          // of key kb + lane, lane < BK
+  PageWindow<BK> win;
+  int block = 0;
+  auto fetch = [&](int kb) __attribute__((always_inline)) {
+    if (block == win.left) {
+      win.load(a.c, it.b, kb, k1);
+      block = 0;
+    }
+    const int at = block * win.per_block;
+    ++block;
+    if (kb + BK <= k1) {
+#pragma unroll
+      for (int x = 0; x < NV; ++x) {       // the RPI <= 8 rows of a load lie in one page
+        const int page = __builtin_amdgcn_readlane(win.entry, at + (win.per_block > 1 ? (RPI * x) >> a.c.shift : 0));
+        const size_t off = (((size_t)page << a.c.shift) + ((kb + RPI * x) & slots)) * row_bytes;
+        kr[x] = *reinterpret_cast<const u32x4*>(Kh + off + lane_off);
+      }
+    } else {                               // rows behind the last key repeat it
+#pragma unroll
+      for (int x = 0; x < NV; ++x) {
+        const int key = min(kb + RPI * x + lane / CPR, k1 - 1);
+        const int page = __shfl(win.entry, at + (win.per_block > 1 ? (key - kb) >> a.c.shift : 0));
+        kr[x] = *reinterpret_cast<const u32x4*>(Kh + (((size_t)page << a.c.shift) + (key & slots)) * row_bytes + 16u * (lane % CPR));
+      }
+    }
+    const int key = min(kb + (lane & (BK - 1)), k1 - 1);
+    const int page = __shfl(win.entry, at + (win.per_block > 1 ? (key - kb) >> a.c.shift : 0));
+    home_next = (((size_t)page * a.Hkv + h) << a.c.shift) + (key & slots);
+    if (a.W_in) w_in = a.W_in[home_next];
+  };
+
+  int kb = k0 + wave * BK;
+  if (kb < k1) {
+    win.load(a.c, it.b, kb, k1);
+    fetch(kb);
+  }
+  for (; kb < k1; kb += kRowWaves * BK) {
+#pragma unroll
+    for (int x = 0; x < NV; ++x) *reinterpret_cast<u32x4*>(tile + (RPI * x + lane / CPR) * LD + 16 * (lane % CPR)) = kr[x];
+    asm volatile("" ::: "memory");         // (a wave's LDS operations execute in program order)
+    const float w = w_in;
+    home = home_next;
+    if (kb + kRowWaves * BK < k1) fetch(kb + kRowWaves * BK);
+    float sum[KT];
+    const bool masked = kb + BK - 1 > all_see;
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt) {
+      frag k[NF];
+#pragma unroll
+      for (int f = 0; f < NF; ++f) k[f] = *reinterpret_cast<const frag*>(tile + (16 * kt + l16) * LD + 64 * f + 16 * grp);
+      sum[kt] = 0.f;
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        const f32x4 s = wt_tile<T, NF>(q[rt], k);
+        float p[4];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) p[x] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x], c2, -ref[rt][x]));
+        if (masked) {
+#pragma unroll
+          for (int x = 0; x < 4; ++x)
+            if (kb + 16 * kt + l16 > last[rt][x]) p[x] = 0.f;
+        }
+        sum[kt] += (p[0] + p[1]) + (p[2] + p[3]);
+      }
+      sum[kt] = groups_sum(sum[kt]);
+    }
+    asm volatile("" ::: "memory");         // the tile is rewritten behind these reads
+    if (lane < BK && kb + lane < k1) a.c.W[home] = (KT == 2 && grp == 1 ? sum[KT - 1] : sum[0]) + (a.W_in ? a.decay * w : 0.f);
+  }
+}
+
+// ---- many rows -----------------------------------------------------------------------------------------------------------
+
+// A wave's keys: lane (key 16 kt + l16, bytes 64 f + 16 grp); behind the last one it is repeated.  home: this lane's keys in the weights.
+template <typename T, int D, int NF, int KT>
+__device__ __forceinline__ void wt_keys(const WeightsArgs& a, const ChunkExtent& e, int b, int h, int kbase, typename WtMath<T>::frag (&kf)[KT][NF],
+                                        size_t (&home)[KT]) {
+  const int lane = threadIdx.x & 63, l16 = lane & 15, grp = lane >> 4;
 #pragma unroll
   for (int kt = 0; kt < KT; ++kt) {
     const int j = min(kbase + 16 * kt + l16, e.len - 1);
@@ -58,10 +200,134 @@ __global__ __launch_bounds__(64 * kWtWaves, 2) void weights_kernel(WeightsArgs a
     home[kt] = (((size_t)page * a.Hkv + h) << a.c.shift) + slot;
     const char* kp = static_cast<const char*>(a.c.K) + (((((size_t)page << a.c.shift) + slot) * a.Hkv + h) * D) * sizeof(T) + 16 * grp;
 #pragma unroll
-    for (int f = 0; f < NF; ++f) kf[kt][f] = __builtin_bit_cast(frag, *reinterpret_cast<const u32x4*>(kp + 64 * f));
+    for (int f = 0; f < NF; ++f) kf[kt][f] = __builtin_bit_cast(typename WtMath<T>::frag, *reinterpret_cast<const u32x4*>(kp + 64 * f));
   }
+}
 
-  // ---- rows that count and see the first of these keys ----
+// One tile of rows against the wave's keys.
+template <typename T, int NF, int KT>
+__device__ __forceinline__ void wt_rows(const typename WtMath<T>::frag (&q)[NF], const typename WtMath<T>::frag (&kf)[KT][NF], const float (&ref)[4],
+                                        const int (&last)[4], bool masked, int kbase, float c2, float (&sum)[KT]) {
+  const int l16 = threadIdx.x & 15;
+#pragma unroll
+  for (int kt = 0; kt < KT; ++kt) {
+    const f32x4 s = wt_tile<T, NF>(q, kf[kt]);
+    float p[4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) p[x] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x], c2, -ref[x]));
+    if (masked) {
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+        if (kbase + 16 * kt + l16 > last[x]) p[x] = 0.f;
+    }
+    sum[kt] += (p[0] + p[1]) + (p[2] + p[3]);
+  }
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(kWtThreads, 2) void weights_block_kernel(WeightsArgs a) {
+  typedef typename WtMath<T>::frag frag;
+  constexpr int RB = D * sizeof(T), NF = RB / 64, KT = wt_tiles<T, D>(), KEYS = 16 * KT;
+  constexpr int CPR = RB / 16, NL = kWtRows * CPR / kWtThreads;         // pieces of a row, loads per thread and turn
+  constexpr int LD = RB + 16;
+  __shared__ __attribute__((aligned(16))) unsigned char rows_lds[2][kWtRows * LD];
+  __shared__ __attribute__((aligned(16))) float ref_lds[2][kWtRows];
+  __shared__ __attribute__((aligned(16))) int last_lds[2][kWtRows];
+
+  const int b = blockIdx.z, h = blockIdx.y, G = a.Hq / a.Hkv, tid = threadIdx.x;
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, grp = lane >> 4;
+  const ChunkExtent e = chunk_extent(a.r, a.c, b);
+  const int kfirst = blockIdx.x * kWtWaves * KEYS;       // of the workgroup
+  if (kfirst >= e.len) return;                           // workgroup-uniform
+  const int kbase = kfirst + wave * KEYS;
+  frag kf[KT][NF];
+  size_t home[KT];
+  wt_keys<T, D, NF, KT>(a, e, b, h, min(kbase, e.len - 1), kf, home);
+
+  // rows that count and see the workgroup's first key
+  const int ctx = e.len - e.n;
+  const int i_lo = max(max(e.n - a.window, kfirst - ctx), 0);
+  const int rows = e.n * G, r_lo = min(i_lo, e.n) * G;
+  const float c2 = a.scale * 1.4426950408889634f;
+  float sum[KT];
+#pragma unroll
+  for (int kt = 0; kt < KT; ++kt) sum[kt] = 0.f;
+
+  u32x4 next[NL];
+  float ref_next = INFINITY;
+  int last_next = 0;
+  auto fetch = [&](int r0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int x = 0; x < NL; ++x) {
+      const int c = tid + kWtThreads * x, row = min(r0 + c / CPR, rows - 1);
+      const int i = row / G, hq = h * G + row - i * G;
+      next[x] = *reinterpret_cast<const u32x4*>(static_cast<const char*>(a.Q) + ((size_t)(e.row0 + i) * a.Hq + hq) * RB + 16 * (c % CPR));
+    }
+    if (tid < kWtRows) {
+      const int row = r0 + tid, i = min(row, rows - 1) / G, hq = h * G + min(row, rows - 1) - i * G;
+      const float x = a.lse[(size_t)hq * a.r.total + e.row0 + i];
+      ref_next = row < rows ? wt_reference(x) : INFINITY;
+      last_next = ctx + i;
+    }
+  };
+  auto place = [&](int buf) __attribute__((always_inline)) {
+#pragma unroll
+    for (int x = 0; x < NL; ++x) {
+      const int c = tid + kWtThreads * x;
+      *reinterpret_cast<u32x4*>(rows_lds[buf] + (c / CPR) * LD + 16 * (c % CPR)) = next[x];
+    }
+    if (tid < kWtRows) {
+      ref_lds[buf][tid] = ref_next;
+      last_lds[buf][tid] = last_next;
+    }
+  };
+  if (r_lo < rows) {
+    fetch(r_lo);
+    place(0);
+  }
+  __syncthreads();
+  int buf = 0;
+  for (int r0 = r_lo; r0 < rows; r0 += kWtRows, buf ^= 1) {
+    if (r0 + kWtRows < rows) fetch(r0 + kWtRows);
+    const bool masked = ctx + r0 / G < kbase + KEYS - 1;
+#pragma unroll
+    for (int rt = 0; rt < kWtRows / 16; ++rt) {
+      frag q[NF];
+#pragma unroll
+      for (int f = 0; f < NF; ++f) q[f] = *reinterpret_cast<const frag*>(rows_lds[buf] + (16 * rt + l16) * LD + 64 * f + 16 * grp);
+      float ref[4];
+      int last[4];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        ref[x] = ref_lds[buf][16 * rt + 4 * grp + x];
+        last[x] = last_lds[buf][16 * rt + 4 * grp + x];
+      }
+      wt_rows<T, NF, KT>(q, kf, ref, last, masked, kbase, c2, sum);
+    }
+    if (r0 + kWtRows < rows) place(buf ^ 1);             // read by nobody since the barrier before
+    __syncthreads();
+  }
+#pragma unroll
+  for (int kt = 0; kt < KT; ++kt) {
+    sum[kt] = groups_sum(sum[kt]);
+    if (grp == 0 && kbase + 16 * kt + l16 < e.len) a.c.W[home[kt]] = sum[kt] + (a.W_in ? a.decay * a.W_in[home[kt]] : 0.f);
+  }
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(kWtThreads, 2) void weights_share_kernel(WeightsArgs a) {
+  typedef typename WtMath<T>::frag frag;
+  constexpr int RB = D * sizeof(T), NF = RB / 64, KT = wt_tiles<T, D>(), KEYS = 16 * KT;
+  __shared__ float sm[kWtWaves][KEYS];
+  const int b = blockIdx.z, h = blockIdx.y, G = a.Hq / a.Hkv;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, grp = lane >> 4;
+  const ChunkExtent e = chunk_extent(a.r, a.c, b);
+  const int kbase = blockIdx.x * KEYS;
+  if (kbase >= e.len) return;              // workgroup-uniform
+  frag kf[KT][NF];
+  size_t home[KT];
+  wt_keys<T, D, NF, KT>(a, e, b, h, kbase, kf, home);
+
   const int ctx = e.len - e.n;
   const int i_lo = max(max(e.n - a.window, kbase - ctx), 0);
   const int rows = e.n * G, r_lo = min(i_lo, e.n) * G;
@@ -69,98 +335,73 @@ __global__ __launch_bounds__(64 * kWtWaves, 2) void weights_kernel(WeightsArgs a
   float sum[KT];
 #pragma unroll
   for (int kt = 0; kt < KT; ++kt) sum[kt] = 0.f;
-
   frag qn[NF];
-  float lse_n = INFINITY;
+  float ref_n = INFINITY;
   int i_n = 0;
   auto fetch = [&](int r0) __attribute__((always_inline)) {
-    const int row = r0 + l16;
-    const bool ok = row < rows;
-    const int i = ok ? row / G : 0, hq = h * G + (ok ? row - i * G : 0);
+    const int row = r0 + l16, at = min(row, rows - 1), i = at / G, hq = h * G + at - i * G;
+    const char* qp = static_cast<const char*>(a.Q) + ((size_t)(e.row0 + i) * a.Hq + hq) * RB + 16 * grp;
+#pragma unroll
+    for (int f = 0; f < NF; ++f) qn[f] = __builtin_bit_cast(frag, *reinterpret_cast<const u32x4*>(qp + 64 * f));
+    const float x = a.lse[(size_t)hq * a.r.total + e.row0 + i];
+    ref_n = row < rows ? wt_reference(x) : INFINITY;
     i_n = i;
-    lse_n = INFINITY;                      // rows that do not exist or see nothing: exp(. - inf) = 0
-    const char* qp = static_cast<const char*>(a.Q) + ((size_t)(e.row0 + i) * a.Hq + hq) * D * sizeof(T) + 16 * grp;
-#pragma unroll
-    for (int f = 0; f < NF; ++f) {
-      u32x4 v = {0, 0, 0, 0};
-      if (ok) v = *reinterpret_cast<const u32x4*>(qp + 64 * f);
-      qn[f] = __builtin_bit_cast(frag, v);
-    }
-    if (ok) {
-      const float x = a.lse[(size_t)hq * a.r.total + e.row0 + i];
-      lse_n = x == -INFINITY ? INFINITY : x * 1.4426950408889634f;
-    }
   };
-  const int step = SHARE ? 16 * kWtWaves : 16;
-  int r0 = r_lo + (SHARE ? 16 * wave : 0);
+  int r0 = r_lo + 16 * wave;
   if (r0 < rows) fetch(r0);
-  for (; r0 < rows; r0 += step) {
+  for (; r0 < rows; r0 += 16 * kWtWaves) {
     frag q[NF];
-#pragma unroll
-    for (int f = 0; f < NF; ++f) q[f] = qn[f];
-    float lse2[4];
+    float ref[4];
     int last[4];
 #pragma unroll
-    for (int x = 0; x < 4; ++x) lse2[x] = __shfl(lse_n, 4 * grp + x);
-    const bool masked = ctx + r0 / G < kbase + KEYS - 1;
-    if (masked) {
+    for (int f = 0; f < NF; ++f) q[f] = qn[f];
 #pragma unroll
-      for (int x = 0; x < 4; ++x) last[x] = ctx + __shfl(i_n, 4 * grp + x);
+    for (int x = 0; x < 4; ++x) {
+      ref[x] = __shfl(ref_n, 4 * grp + x);
+      last[x] = ctx + __shfl(i_n, 4 * grp + x);
     }
-    if (r0 + step < rows) fetch(r0 + step);
-#pragma unroll
-    for (int kt = 0; kt < KT; ++kt) {
-      f32x4 acc[M::CH];
-#pragma unroll
-      for (int c = 0; c < M::CH; ++c) acc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int f = 0; f < NF; ++f) M::mma(acc, q[f], kf[kt][f]);
-#pragma unroll
-      for (int half = M::CH / 2; half; half /= 2)
-#pragma unroll
-        for (int c = 0; c < half; ++c) acc[c] += acc[c + half];
-      float p[4];
-#pragma unroll
-      for (int x = 0; x < 4; ++x) p[x] = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[0][x], c2, -lse2[x]));
-      if (masked) {
-#pragma unroll
-        for (int x = 0; x < 4; ++x)
-          if (kbase + 16 * kt + l16 > last[x]) p[x] = 0.f;
-      }
-      sum[kt] += (p[0] + p[1]) + (p[2] + p[3]);
-    }
-  }
-
-#pragma unroll
-  for (int kt = 0; kt < KT; ++kt) sum[kt] = groups_sum(sum[kt]);
-  if (SHARE) {
-    if (grp == 0) {
-#pragma unroll
-      for (int kt = 0; kt < KT; ++kt) sm[wave][16 * kt + l16] = sum[kt];
-    }
-    __syncthreads();
-    if (wave != 0) return;
-#pragma unroll
-    for (int kt = 0; kt < KT; ++kt) {
-      sum[kt] = 0.f;
-#pragma unroll
-      for (int w = 0; w < kWtWaves; ++w) sum[kt] += sm[SHARE ? w : 0][SHARE ? 16 * kt + l16 : 0];
-    }
+    if (r0 + 16 * kWtWaves < rows) fetch(r0 + 16 * kWtWaves);
+    wt_rows<T, NF, KT>(q, kf, ref, last, ctx + r0 / G < kbase + KEYS - 1, kbase, c2, sum);
   }
 #pragma unroll
-  for (int kt = 0; kt < KT; ++kt)
-    if (grp == 0 && kbase + 16 * kt + l16 < e.len)
-      a.c.W[home[kt]] = sum[kt] + (a.W_in ? a.decay * a.W_in[home[kt]] : 0.f);
+  for (int kt = 0; kt < KT; ++kt) {
+    sum[kt] = groups_sum(sum[kt]);
+    if (grp == 0) sm[wave][16 * kt + l16] = sum[kt];
+  }
+  __syncthreads();
+  if (wave != 0 || grp != 0) return;
+#pragma unroll
+  for (int kt = 0; kt < KT; ++kt) {
+    float s = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWtWaves; ++w) s += sm[w][16 * kt + l16];
+    if (kbase + 16 * kt + l16 < e.len) a.c.W[home[kt]] = s + (a.W_in ? a.decay * a.W_in[home[kt]] : 0.f);
+  }
 }
 
 template <typename T, int D>
-hipError_t launch(const WeightsArgs& a, hipStream_t s) {
-  // few rows: the keys are the work, every wave has its own
-  const bool share = (long long)std::min(std::min(a.r.max_q, a.window), a.r.total) * (a.Hq / a.Hkv) > 64;
-  const int keys = 16 * kWtTiles * (share ? 1 : kWtWaves);
-  const dim3 grid((a.c.cap + keys - 1) / keys, a.Hkv, a.r.B), block(64 * kWtWaves);
-  if (share) hipLaunchKernelGGL((weights_kernel<T, D, true>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((weights_kernel<T, D, false>), grid, block, 0, s, a);
+hipError_t launch(WeightsArgs a, hipStream_t s) {
+  const long long rows = (long long)std::min(std::min(a.r.max_q, a.window), a.r.total) * (a.Hq / a.Hkv);
+  const dim3 threads(kWtThreads);
+  constexpr int kFew = D * sizeof(T) > 256 ? 32 : 64;      // rows that the streaming kernel's registers hold
+  if (rows <= kFew) {
+    a.p.R = 0;
+    a.p.G = a.Hq / a.Hkv;
+    a.p.slots_log2 = 0;
+    while ((1 << a.p.slots_log2) * a.Hkv < 1024) ++a.p.slots_log2;
+    a.p.least = 8;
+    a.p.max_splits = std::max(1, (a.c.cap + 255) / 256);
+    const int items = (int)std::min((long long)a.r.B + (1 << a.p.slots_log2), (long long)a.r.B * a.p.max_splits);
+    const dim3 grid(items, a.Hkv);
+    if (rows <= 16) hipLaunchKernelGGL((weights_stream_kernel<T, D, 1>), grid, dim3(64 * kRowWaves), 0, s, a);
+    else if (rows <= 32) hipLaunchKernelGGL((weights_stream_kernel<T, D, 2>), grid, dim3(64 * kRowWaves), 0, s, a);
+    else hipLaunchKernelGGL((weights_stream_kernel<T, D, kFew / 16>), grid, dim3(64 * kRowWaves), 0, s, a);
+    return hipGetLastError();
+  }
+  constexpr int KEYS = 16 * wt_tiles<T, D>();
+  const int blocks = (a.c.cap + KEYS * kWtWaves - 1) / (KEYS * kWtWaves);
+  if ((long long)blocks * a.Hkv * a.r.B >= 256) hipLaunchKernelGGL((weights_block_kernel<T, D>), dim3(blocks, a.Hkv, a.r.B), threads, 0, s, a);
+  else hipLaunchKernelGGL((weights_share_kernel<T, D>), dim3((a.c.cap + KEYS - 1) / KEYS, a.Hkv, a.r.B), threads, 0, s, a);
   return hipGetLastError();
 }
 
