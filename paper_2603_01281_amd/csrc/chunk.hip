@@ -21,7 +21,7 @@ typedef __attribute__((address_space(3))) s16x4* row_lds_s16x4_ptr;
 typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
 
 template <int D, int RT>
-__global__ __launch_bounds__(kRowThreads, 2) void chunk_rows_bf16_kernel(ChunkArgs a) {
+__global__ __launch_bounds__(kRowThreads, RT == 4 && D == 128 ? 1 : 2) void chunk_rows_bf16_kernel(ChunkArgs a) {
   constexpr int BK = 32, R = 16 * RT;
   // LDS row strides (elements): 16 rows of K at one 16-byte column, and 16 rows x 32 bytes of V, spread over all banks
   constexpr int LDK = D + 8, LDV = D + 16, OLD = D + 4;
@@ -33,7 +33,9 @@ __global__ __launch_bounds__(kRowThreads, 2) void chunk_rows_bf16_kernel(ChunkAr
   __shared__ float sm_ml[kRowWaves][16][2];
 
   ChunkItem it;
-  if (!plan_item<false>(a.r, a.c, a.p, blockIdx.x, it)) return;         // workgroup-uniform
+  const bool exists = plan_item(a.r, a.c, a.p, blockIdx.x, it);
+  row_describe(a, exists, it);
+  if (!exists) return;                     // workgroup-uniform
   int k0, k1;
   plan_range(a.p, it, k0, k1);
   const int h = blockIdx.y, G = a.p.G;
@@ -79,7 +81,8 @@ __global__ __launch_bounds__(kRowThreads, 2) void chunk_rows_bf16_kernel(ChunkAr
   u32x4 kr[NV], vr[NV];
   PageWindow<BK> win;
   int block = 0;                           // of the window
-  auto fetch = [&](int kb) __attribute__((always_inline)) {
+  auto fetch = [&](auto nt, int kb) __attribute__((always_inline)) {
+    constexpr bool NT = decltype(nt)::value;
     if (block == win.left) {
       win.load(a.c, it.b, kb, k1);
       block = 0;
@@ -91,8 +94,8 @@ __global__ __launch_bounds__(kRowThreads, 2) void chunk_rows_bf16_kernel(ChunkAr
       for (int x = 0; x < NV; ++x) {       // the RPI <= 8 rows of a load lie in one page
         const int page = __builtin_amdgcn_readlane(win.entry, at + (win.per_block > 1 ? (RPI * x) >> a.c.shift : 0));
         const size_t off = (((size_t)page << a.c.shift) + ((kb + RPI * x) & slots)) * row_bytes;
-        kr[x] = *reinterpret_cast<const u32x4*>(Kh + off + lane_off);
-        vr[x] = *reinterpret_cast<const u32x4*>(Vh + off + lane_off);
+        kr[x] = paged_load<NT>(reinterpret_cast<const u32x4*>(Kh + off + lane_off));
+        vr[x] = paged_load<NT>(reinterpret_cast<const u32x4*>(Vh + off + lane_off));
       }
     } else {                               // rows behind the last key repeat it
 #pragma unroll
@@ -100,16 +103,17 @@ __global__ __launch_bounds__(kRowThreads, 2) void chunk_rows_bf16_kernel(ChunkAr
         const int key = min(kb + RPI * x + lane / CPR, k1 - 1);
         const int page = __shfl(win.entry, at + (win.per_block > 1 ? (key - kb) >> a.c.shift : 0));
         const size_t off = (((size_t)page << a.c.shift) + (key & slots)) * row_bytes + 16u * (lane % CPR);
-        kr[x] = *reinterpret_cast<const u32x4*>(Kh + off);
-        vr[x] = *reinterpret_cast<const u32x4*>(Vh + off);
+        kr[x] = paged_load<NT>(reinterpret_cast<const u32x4*>(Kh + off));
+        vr[x] = paged_load<NT>(reinterpret_cast<const u32x4*>(Vh + off));
       }
     }
   };
 
+  auto run = [&](auto nt) __attribute__((always_inline)) {
   int kb = k0 + wave * BK;
   if (kb < k1) {
     win.load(a.c, it.b, kb, k1);
-    fetch(kb);
+    fetch(nt, kb);
   }
   for (; kb < k1; kb += kRowWaves * BK) {
     // (a wave's LDS operations execute in program order; the fences are for the compiler)
@@ -134,7 +138,7 @@ __global__ __launch_bounds__(kRowThreads, 2) void chunk_rows_bf16_kernel(ChunkAr
     for (int x = 0; x < NV; ++x) *reinterpret_cast<u32x4*>(tile + (RPI * x + lane / CPR) * LDV + 8 * (lane % CPR)) = vr[x];
     asm volatile("" ::: "memory");
     const int kb_next = kb + kRowWaves * BK;
-    if (kb_next < k1) fetch(kb_next);      // on their way during the softmax
+    if (kb_next < k1) fetch(nt, kb_next);      // on their way during the softmax
 
     bf16x8 pb[RT];
     const bool masked = kb + BK - 1 > all_see || kb + BK > k1;
@@ -179,6 +183,9 @@ __global__ __launch_bounds__(kRowThreads, 2) void chunk_rows_bf16_kernel(ChunkAr
     }
     asm volatile("" ::: "memory");         // the tile is rewritten behind these reads
   }
+  };
+  if (it.streams) run(std::true_type{});
+  else run(std::false_type{});
 
   // ---- merge the waves, 16 rows at a time; lane (row l16, grp) holds O[row][16 dt + 4 grp + i] ----
 #pragma unroll
@@ -198,12 +205,12 @@ __global__ __launch_bounds__(kRowThreads, 2) void chunk_rows_bf16_kernel(ChunkAr
 }
 
 template <int D>
-hipError_t launch_rows(const ChunkArgs& a, int rows16, int items, int chunks, hipStream_t s) {
+hipError_t launch_rows(const ChunkArgs& a, int rows16, int items, int rows, hipStream_t s) {
   const dim3 grid(items, a.Hkv), block(kRowThreads);
   if (rows16 == 1) hipLaunchKernelGGL((chunk_rows_bf16_kernel<D, 1>), grid, block, 0, s, a);
   else if (rows16 == 2) hipLaunchKernelGGL((chunk_rows_bf16_kernel<D, 2>), grid, block, 0, s, a);
   else hipLaunchKernelGGL((chunk_rows_bf16_kernel<D, 4>), grid, block, 0, s, a);
-  if (a.p.max_splits > 1) hipLaunchKernelGGL((chunk_merge_kernel<uint16_t, D>), dim3(chunks, a.Hkv), dim3(256), 0, s, a);
+  launch_chunk_merge<uint16_t, D>(a, items, rows, s);
   return hipGetLastError();
 }
 
@@ -211,24 +218,26 @@ hipError_t launch_rows(const ChunkArgs& a, int rows16, int items, int chunks, hi
 // has more than max_q, caches of up to S tokens.
 struct RowPlan {
   ChunkPlan p;
-  int rows16, chunks, items;
+  int rows16, rows, items;               // tiles of 16 rows, rows that a chunk can have, items
 };
-RowPlan row_plan(int B, int S, int Hq, int Hkv, int dtype, int total, int max_q) {
+RowPlan row_plan(int B, int S, int Hq, int Hkv, int D, int dtype, int total, int max_q) {
   RowPlan r;
   const int G = Hq / Hkv;
   const long long rows = (long long)std::min(max_q, total) * G;
   r.rows16 = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
   r.p.R = 16 * r.rows16;
   r.p.G = G;
-  r.chunks = (int)std::min(((long long)total * G) / r.p.R + B, (long long)0x3fffffff);
+  r.rows = (int)std::min(rows, (long long)r.p.R);
+  const int chunks = (int)std::min(((long long)total * G) / r.p.R + B, (long long)0x3fffffff);
   // two workgroups of four waves to a compute unit, about
   r.p.slots_log2 = 0;
   while ((1 << r.p.slots_log2) * Hkv < 512) ++r.p.slots_log2;
   r.p.least = 8;                           // 256 tokens
+  r.p.streams = (long long)(300e6 / (2.0 * 32 * Hkv * D * (dtype == SEKA_BF16 ? 2 : 4)));
   const int blocks = (S + 31) / 32;
-  r.p.max_splits = std::max(1, std::min(64, (blocks + r.p.least - 1) / r.p.least));
+  r.p.max_splits = std::max(1, std::min(kMaxRanges, (blocks + r.p.least - 1) / r.p.least));
   // sum over chunks of ceil(blocks / L) <= T / L + chunks with T / L <= slots, and no more than every chunk in all its ranges
-  r.items = (int)std::min((long long)r.chunks + (1 << r.p.slots_log2), (long long)r.chunks * r.p.max_splits);
+  r.items = (int)std::min((long long)chunks + (1 << r.p.slots_log2), (long long)chunks * r.p.max_splits);
   return r;
 }
 
@@ -259,14 +268,16 @@ bool pipe_plan(int S, int Hq, int Hkv, int D, int dtype, int shift, int total, i
 
 }  // namespace
 
-hipError_t launch_chunk_bf16(const ChunkArgs& a, int D, int rows16, int items, int chunks, hipStream_t s) {
-  return D == 128 ? launch_rows<128>(a, rows16, items, chunks, s) : launch_rows<64>(a, rows16, items, chunks, s);
+hipError_t launch_chunk_bf16(const ChunkArgs& a, int D, int rows16, int items, int rows, hipStream_t s) {
+  return D == 128 ? launch_rows<128>(a, rows16, items, rows, s) : launch_rows<64>(a, rows16, items, rows, s);
 }
+
+size_t row_states(const RowPlan& r, int Hkv, int D) { return r.p.max_splits > 1 ? (size_t)r.items * Hkv * r.p.R * (D + 4) * sizeof(float) : 0; }
 
 // (the larger need: which kernel runs depends on the page size too)
 size_t chunk_workspace_bytes(int B, int S, int Hq, int Hkv, int D, int dtype, int total, int max_q) {
-  const RowPlan r = row_plan(B, S, Hq, Hkv, dtype, total, max_q);
-  const size_t rows = r.p.max_splits > 1 ? (size_t)r.items * Hkv * r.p.R * (D + 4) * sizeof(float) : 0;
+  const RowPlan r = row_plan(B, S, Hq, Hkv, D, dtype, total, max_q);
+  const size_t rows = row_states(r, Hkv, D) + (size_t)r.items * sizeof(int4);
   PipeChunkPlan p;
   return pipe_plan(S, Hq, Hkv, D, dtype, 16, total, max_q, &p) ? std::max(rows, p.workspace) : rows;
 }
@@ -278,10 +289,10 @@ hipError_t launch_chunk(ChunkArgs a, int D, int dtype, int S, hipStream_t s) {
     a.cuts = reinterpret_cast<int4*>(reinterpret_cast<char*>(a.part) + p.cuts);
     return D == 128 ? launch_chunk_pipe_d128(a, p, s) : launch_chunk_pipe_d64(a, p, s);
   }
-  const RowPlan r = row_plan(a.r.B, S, a.Hq, a.Hkv, dtype, a.r.total, a.r.max_q);
+  const RowPlan r = row_plan(a.r.B, S, a.Hq, a.Hkv, D, dtype, a.r.total, a.r.max_q);
   a.p = r.p;
-  a.items = r.items;
-  return dtype == SEKA_BF16 ? launch_chunk_bf16(a, D, r.rows16, r.items, r.chunks, s) : launch_chunk_f32(a, D, r.rows16, r.items, r.chunks, s);
+  a.items_of = reinterpret_cast<int4*>(reinterpret_cast<char*>(a.part) + row_states(r, a.Hkv, D));
+  return dtype == SEKA_BF16 ? launch_chunk_bf16(a, D, r.rows16, r.items, r.rows, s) : launch_chunk_f32(a, D, r.rows16, r.items, r.rows, s);
 }
 
 }  // namespace seka

@@ -20,7 +20,9 @@ __global__ __launch_bounds__(kRowThreads, RT == 4 ? 1 : 2) void chunk_rows_f32_k
   __shared__ float sm_ml[kRowWaves][16][2];
 
   ChunkItem it;
-  if (!plan_item<false>(a.r, a.c, a.p, blockIdx.x, it)) return;         // workgroup-uniform
+  const bool exists = plan_item(a.r, a.c, a.p, blockIdx.x, it);
+  row_describe(a, exists, it);
+  if (!exists) return;                     // workgroup-uniform
   int k0, k1;
   plan_range(a.p, it, k0, k1);
   const int h = blockIdx.y, G = a.p.G;
@@ -171,19 +173,19 @@ __global__ __launch_bounds__(kRowThreads, RT == 4 ? 1 : 2) void chunk_rows_f32_k
 }
 
 template <int D>
-hipError_t launch_rows(const ChunkArgs& a, int rows16, int items, int chunks, hipStream_t s) {
+hipError_t launch_rows(const ChunkArgs& a, int rows16, int items, int rows, hipStream_t s) {
   const dim3 grid(items, a.Hkv), block(kRowThreads);
   if (rows16 == 1) hipLaunchKernelGGL((chunk_rows_f32_kernel<D, 1>), grid, block, 0, s, a);
   else if (rows16 == 2) hipLaunchKernelGGL((chunk_rows_f32_kernel<D, 2>), grid, block, 0, s, a);
   else hipLaunchKernelGGL((chunk_rows_f32_kernel<D, 4>), grid, block, 0, s, a);
-  if (a.p.max_splits > 1) hipLaunchKernelGGL((chunk_merge_kernel<float, D>), dim3(chunks, a.Hkv), dim3(256), 0, s, a);
+  launch_chunk_merge<float, D>(a, items, rows, s);
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_chunk_f32(const ChunkArgs& a, int D, int rows16, int items, int chunks, hipStream_t s) {
-  return D == 128 ? launch_rows<128>(a, rows16, items, chunks, s) : launch_rows<64>(a, rows16, items, chunks, s);
+hipError_t launch_chunk_f32(const ChunkArgs& a, int D, int rows16, int items, int rows, hipStream_t s) {
+  return D == 128 ? launch_rows<128>(a, rows16, items, rows, s) : launch_rows<64>(a, rows16, items, rows, s);
 }
 
 }  // namespace seka

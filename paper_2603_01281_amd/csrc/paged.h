@@ -42,18 +42,20 @@ __device__ __forceinline__ int page_of(const PagedCache& c, int b, int j) {
 
 // ---- how the rows and keys of a batch are dealt to workgroups -----------------------------------------------------------
 // A request's rows (new token i, head g of the KV head's group: row i G + g) are cut into chunks of R; a chunk's keys are cut
-// into `splits` ranges.  All workgroups find their item from the lengths by themselves, in integers, so that every kernel
-// of a call sees the same plan.  T = sum over chunks of their keys (in blocks of 32); a range has about T / slots blocks
+// into `splits` ranges.  All workgroups find their item from the lengths by themselves, in integers, so that every workgroup
+// sees the same plan.  T = sum over chunks of their keys (in blocks of 32); a range has about T / slots blocks
 // and no fewer than least; slots is a power of two.
 struct ChunkPlan {
   int R, G;               // rows per chunk, query heads per KV head; R = 0: one chunk for every request that has cached tokens
   int slots_log2;         // about so many ranges in all, per KV head
   int least;              // blocks of 32 keys in a range, at least
   int max_splits;
+  long long streams;      // more blocks than this in all: the keys and values are not kept in the caches
 };
 
 struct ChunkItem {
-  int b, rc, split, splits, index;      // index: where the partial states of this item lie
+  int b, rc, split, splits;
+  bool streams;
   ChunkExtent e;
 };
 
@@ -67,8 +69,7 @@ __device__ __forceinline__ int plan_scan(int v) {       // inclusive sum over th
   return v;
 }
 
-// BY_CHUNK: item counts chunks, and split is 0 (the merge kernel); otherwise it counts (chunk, range).  Wave-uniform; false: no such item.
-template <bool BY_CHUNK>
+// The item-th (chunk, range).  Wave-uniform; false: no such item.
 __device__ __forceinline__ bool plan_item(const ChunkRows& r, const PagedCache& c, const ChunkPlan& p, int item, ChunkItem& out) {
   const int lane = threadIdx.x & 63;
   ChunkExtent e = {0, 0, 0};
@@ -90,33 +91,30 @@ __device__ __forceinline__ bool plan_item(const ChunkRows& r, const PagedCache& 
     for (int d = 1; d < 64; d <<= 1) w += __shfl_xor(w, d);
     T += w;
   }
+  out.streams = T > (unsigned long long)p.streams;
   const unsigned long long per = (T + (1ull << p.slots_log2) - 1) >> p.slots_log2;
   const int L = (int)max((unsigned long long)p.least, min(per, 0x7fffffffull));
-  int before = 0, before_items = 0;      // chunks and items of the requests already passed
+  int before = 0;                        // items of the requests already passed
   for (int b0 = 0; b0 < r.B; b0 += 64) {
     if (r.B > 64) look(b0);
     const int splits = max(1, min((blocks + L - 1) / L, p.max_splits));
-    const int items = chunks * splits;
-    const int ends = plan_scan(items), cends = BY_CHUNK ? plan_scan(chunks) : ends;
-    const int first = (BY_CHUNK ? before + cends - chunks : before_items + ends - items);
-    const int mine = BY_CHUNK ? chunks : items;
-    const unsigned long long hit = __ballot(item >= first && item < first + mine);
+    const int items = chunks * splits, ends = plan_scan(items);
+    const int first = before + ends - items;
+    const unsigned long long hit = __ballot(item >= first && item < first + items);
     if (hit != 0ull) {
       const int at = __builtin_ctzll(hit);
       const int local = item - __builtin_amdgcn_readlane(first, at);
       const int s = __builtin_amdgcn_readlane(splits, at);
       out.b = b0 + at;
       out.splits = s;
-      out.rc = BY_CHUNK ? local : local / s;
-      out.split = BY_CHUNK ? 0 : local % s;
-      out.index = before_items + __builtin_amdgcn_readlane(ends - items, at) + out.rc * s + out.split;
+      out.rc = local / s;
+      out.split = local % s;
       out.e.row0 = __builtin_amdgcn_readlane(e.row0, at);
       out.e.n = __builtin_amdgcn_readlane(e.n, at);
       out.e.len = __builtin_amdgcn_readlane(e.len, at);
       return true;
     }
-    before_items += __builtin_amdgcn_readlane(ends, 63);
-    before += __builtin_amdgcn_readlane(cends, 63);
+    before += __builtin_amdgcn_readlane(ends, 63);
   }
   return false;
 }
@@ -165,6 +163,13 @@ struct PageWindow {
   }
 };
 
+// NT: a load that keeps no place for its line in the caches.
+template <bool NT, typename V>
+__device__ __forceinline__ V paged_load(const V* p) {
+  if constexpr (NT) return __builtin_nontemporal_load(p);
+  else return *p;
+}
+
 struct ChunkArgs {
   const void* Q;
   void* O;
@@ -172,7 +177,7 @@ struct ChunkArgs {
   PagedCache c;
   ChunkRows r;
   ChunkPlan p;
-  int items;              // (chunk, range) pairs that are launched and have room in part
+  int4* items_of;         // few rows: what the joining kernel has to know of each item
   float* part;            // partial states: [item, Hkv, R, D + 4]: outputs, reference exponent (base 2), sum
   int Hq, Hkv;
   int width;              // long chunks: workgroups per head chunk (chunk_plan.h)

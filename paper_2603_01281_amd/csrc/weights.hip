@@ -74,7 +74,7 @@ __global__ __launch_bounds__(kRowWaves * 64, 2) void weights_stream_kernel(Weigh
   __shared__ __attribute__((aligned(16))) unsigned char smem[kRowWaves * BK * LD];
 
   ChunkItem it;
-  if (!plan_item<false>(a.r, a.c, a.p, blockIdx.x, it)) return;
+  if (!plan_item(a.r, a.c, a.p, blockIdx.x, it)) return;
   int k0, k1;
   plan_range(a.p, it, k0, k1);
   const int h = blockIdx.y, G = a.Hq / a.Hkv;
