@@ -16,8 +16,8 @@ namespace {
 
 constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64;
 constexpr int kSelCopies = 16;                  // of every counter: lanes that count the same byte meet in one of them
-constexpr int kSelKeys = 32 * 1024;             // tokens whose keys LDS holds
-constexpr int kMoveThreads = 256;
+constexpr int kSelKeys = 30 * 1024;             // tokens whose keys LDS holds
+constexpr int kMoveThreads = 256, kMoveRows = 4;     // rows of a thread whose pieces are in flight together
 
 // Larger weights have larger keys; both zeros the same one; what is not a number the smallest.
 __device__ __forceinline__ uint32_t weight_key(float w) {
@@ -28,8 +28,8 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
 
 __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(EvictArgs a) {
   extern __shared__ uint32_t keys[];            // [min(candidates, kSelKeys)]
-  __shared__ uint32_t hist[256 * kSelCopies];
-  __shared__ uint32_t sm_found[2];              // byte, how many above it
+  __shared__ __attribute__((aligned(16))) uint32_t hist[2][256 * kSelCopies];
+  __shared__ __attribute__((aligned(16))) uint32_t total[2][256];
   __shared__ int sm_gt[kSelWaves], sm_eq[kSelWaves];
   const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int n = min(max(a.src.lens[b], 0), a.src.cap);
@@ -44,55 +44,69 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(EvictArgs a) 
   if (want == 0) return;
   const int shift = a.src.shift;
   const bool held = m <= kSelKeys;
-  auto key_at = [&](int j) __attribute__((always_inline)) -> uint32_t {
-    if (held) return keys[j];
-    return weight_key(a.src.W[(((size_t)page_of(a.src, b, j) * a.Hkv + h) << shift) + (j & ((1 << shift) - 1))]);
+  auto weight_at = [&](int j) __attribute__((always_inline)) -> float {
+    return a.src.W[(((size_t)page_of(a.src, b, j) * a.Hkv + h) << shift) + (j & ((1 << shift) - 1))];
   };
+  auto key_at = [&](int j) __attribute__((always_inline)) -> uint32_t { return held ? keys[j] : weight_key(weight_at(j)); };
   if (held) {
-    for (int j = tid; j < m; j += kSelThreads)
-      keys[j] = weight_key(a.src.W[(((size_t)page_of(a.src, b, j) * a.Hkv + h) << shift) + (j & ((1 << shift) - 1))]);
+    constexpr int U = 8;                        // tokens of a thread whose loads are in flight together
+    for (int j0 = tid; j0 < m; j0 += U * kSelThreads) {
+      float w[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) w[u] = weight_at(min(j0 + u * kSelThreads, m - 1));
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (j0 + u * kSelThreads < m) keys[j0 + u * kSelThreads] = weight_key(w[u]);
+    }
   }
+  for (int k = tid; k < 256 * kSelCopies; k += kSelThreads) hist[0][k] = 0;
+  __syncthreads();
   // ---- the want-th largest key, a byte at a time ----
   uint32_t prefix = 0;
   int need = want;                              // of the keys that begin with prefix
   for (int byte = 3; byte >= 0; --byte) {
-    for (int k = tid; k < 256 * kSelCopies; k += kSelThreads) hist[k] = 0;
-    __syncthreads();
+    const int now = byte & 1 ? 0 : 1;           // counters of this byte; the others are cleared for the next one
+#pragma unroll 4
     for (int j = tid; j < m; j += kSelThreads) {
       const uint32_t u = key_at(j);
-      if (byte == 3 || (u >> (8 * byte + 8)) == prefix) atomicAdd(&hist[((u >> (8 * byte)) & 255) * kSelCopies + (lane & (kSelCopies - 1))], 1u);
+      if (byte == 3 || (u >> (8 * byte + 8)) == prefix) atomicAdd(&hist[now][((u >> (8 * byte)) & 255) * kSelCopies + (lane & (kSelCopies - 1))], 1u);
     }
     __syncthreads();
-    if (wave == 0) {                            // lane l: the bytes 255 - 4 l .. 252 - 4 l, the largest first
-      uint32_t c[4], mine = 0;
+    {                                           // four threads to a counter, four copies each
+      uint32_t c = 0;
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        c[x] = 0;
-        for (int k = 0; k < kSelCopies; ++k) c[x] += hist[(255 - 4 * lane - x) * kSelCopies + k];
-        mine += c[x];
-      }
-      uint32_t upto = mine;
+      for (int k = 0; k < 4; ++k) c += hist[now][4 * tid + k];
+      c += __shfl_xor(c, 1);
+      c += __shfl_xor(c, 2);
+      if ((tid & 3) == 0) total[now][tid >> 2] = c;
 #pragma unroll
-      for (int d = 1; d < 64; d <<= 1) {
-        const uint32_t o = __shfl_up(upto, d);
-        if (lane >= d) upto += o;
-      }
-      uint32_t above = upto - mine;
-      if ((int)above < need && need <= (int)upto) {       // in one lane
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          if ((int)above < need && need <= (int)(above + c[x])) {
-            sm_found[0] = 255 - 4 * lane - x;
-            sm_found[1] = above;
-          }
-          above += c[x];
-        }
-      }
+      for (int k = 0; k < 4; ++k) hist[now ^ 1][4 * tid + k] = 0;
     }
     __syncthreads();
-    prefix = prefix << 8 | sm_found[0];
-    need -= (int)sm_found[1];
-    __syncthreads();
+    // every wave finds the byte by itself; lane l: the bytes 255 - 4 l .. 252 - 4 l, the largest first
+    uint32_t c[4], mine = 0;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) mine += c[x] = total[now][255 - 4 * lane - x];
+    uint32_t above = mine;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const uint32_t o = __shfl_up(above, d);
+      if (lane >= d) above += o;
+    }
+    const unsigned long long hit = __ballot((int)above >= need);       // the first lane that reaches it
+    const int at = __builtin_ctzll(hit);
+    above = __shfl(above - mine, at);
+    uint32_t digit = 255 - 4 * at;
+#pragma unroll
+    for (int x = 0; x < 3; ++x) {
+      const uint32_t cx = __shfl(c[x], at);
+      if (digit == 255u - 4 * at - x && (int)(above + cx) < need) {
+        above += cx;
+        --digit;
+      }
+    }
+    prefix = prefix << 8 | digit;
+    need -= (int)above;
   }
   // ---- every key above prefix, and the first `need` that equal it, in order ----
   const int per = ((m + kSelWaves - 1) / kSelWaves + 63) / 64 * 64;
@@ -164,17 +178,32 @@ __global__ __launch_bounds__(IN_ORDER ? 1024 : kMoveThreads) void evict_move_ker
       if (k < m) *reinterpret_cast<u32x4*>(dst + to(k) * a.row_bytes + off) = v;
     }
   } else {
+    constexpr int U = kMoveRows;
     const int pieces = a.row_bytes / 16, rows = kMoveThreads / pieces;
     const size_t off = 16 * (tid % pieces);
-    for (int k = blockIdx.x * rows + tid / pieces; k < m; k += gridDim.x * rows) {
-      const int j = kept[k];
-      const size_t s0 = from(j) * a.row_bytes + off, d0 = to(k) * a.row_bytes + off;
-      const u32x4 x = *reinterpret_cast<const u32x4*>(static_cast<const char*>(a.src.K) + s0);
-      const u32x4 y = *reinterpret_cast<const u32x4*>(static_cast<const char*>(a.src.V) + s0);
-      *reinterpret_cast<u32x4*>(static_cast<char*>(a.dst.K) + d0) = x;
-      *reinterpret_cast<u32x4*>(static_cast<char*>(a.dst.V) + d0) = y;
-      if (tid % pieces == 0) a.dst.W[w_to(k)] = a.src.W[w_from(j)];
+    for (int k0 = blockIdx.x * rows * U + tid / pieces; k0 < m; k0 += gridDim.x * rows * U) {
+      u32x4 x[U], y[U];
+      int j[U];
+      size_t d[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) j[u] = kept[min(k0 + u * rows, m - 1)];
+#pragma unroll
+      for (int u = 0; u < U; ++u) d[u] = to(min(k0 + u * rows, m - 1)) * a.row_bytes + off;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const size_t s0 = from(j[u]) * a.row_bytes + off;
+        x[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(static_cast<const char*>(a.src.K) + s0));
+        y[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(static_cast<const char*>(a.src.V) + s0));
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (k0 + u * rows < m) {
+          __builtin_nontemporal_store(x[u], reinterpret_cast<u32x4*>(static_cast<char*>(a.dst.K) + d[u]));
+          __builtin_nontemporal_store(y[u], reinterpret_cast<u32x4*>(static_cast<char*>(a.dst.V) + d[u]));
+        }
     }
+    // the weights, one per thread
+    for (int k = blockIdx.x * kMoveThreads + tid; k < m; k += gridDim.x * kMoveThreads) a.dst.W[w_to(k)] = a.src.W[w_from(kept[k])];
   }
 }
 
@@ -191,7 +220,7 @@ hipError_t launch_evict(const EvictArgs& a, hipStream_t s) {
     const int parts = a.row_bytes / 64;                   // pieces of 64 bytes
     hipLaunchKernelGGL((evict_move_kernel<true>), dim3(2 * parts + 1, a.Hkv, a.B), dim3(1024), 0, s, a, parts);
   } else {
-    const int rows = kMoveThreads / (a.row_bytes / 16), most_rows = std::min(a.budget, a.src.cap);
+    const int rows = kMoveThreads / (a.row_bytes / 16) * kMoveRows, most_rows = std::min(a.budget, a.src.cap);
     const int share = std::max(1, std::min((most_rows + rows - 1) / rows, 4096 / std::max(1, a.Hkv * a.B)));
     hipLaunchKernelGGL((evict_move_kernel<false>), dim3(share, a.Hkv, a.B), dim3(kMoveThreads), 0, s, a, 1);
   }

@@ -11,7 +11,8 @@
 // through a wave-private LDS tile, a block ahead, over ranges that are cut as for the attention itself (paged.h, plan_item).
 // Many rows: bound by the vector unit (an exponential takes it four times as long as a multiplication; 96 cycles per tile of 16 x 16
 // against 64 of the matrix pipe at D = 128).  weights_block_kernel holds 64 keys per wave in registers and passes the rows by, 64 at a
-// time through LDS for all its waves.  weights_share_kernel, where those would leave compute units idle: 64 keys per workgroup,
+// time through LDS for all its waves; two groups of four waves have the same keys and take half of the rows each (one wave per SIMD had
+// nothing to hide its latencies behind: a chunk of 1000 over 8192, 32 / 8 heads, 142 us).  weights_share_kernel, where those would leave compute units idle: 64 keys per workgroup,
 // every wave its share of the rows, straight from the caches; the waves' sums are joined in LDS.
 #include <algorithm>
 
@@ -25,6 +26,7 @@ constexpr int kWtWaves = 4, kWtThreads = 64 * kWtWaves;
 // tiles of 16 keys that a wave holds (four of fp32 rows of 512 bytes did not fit its registers)
 template <typename T, int D> constexpr int wt_tiles() { return D * sizeof(T) > 256 ? 2 : 4; }
 constexpr int kWtRows = 64;                     // rows that pass through LDS at a time
+constexpr int kWtGroups = 2, kWtBlockThreads = kWtThreads * kWtGroups;      // of waves with the same keys, each with its share of those rows
 
 template <typename T> struct WtMath;
 template <> struct WtMath<uint16_t> {
@@ -225,17 +227,18 @@ __device__ __forceinline__ void wt_rows(const typename WtMath<T>::frag (&q)[NF],
 }
 
 template <typename T, int D>
-__global__ __launch_bounds__(kWtThreads, 2) void weights_block_kernel(WeightsArgs a) {
+__global__ __launch_bounds__(kWtBlockThreads, 2) void weights_block_kernel(WeightsArgs a) {
   typedef typename WtMath<T>::frag frag;
   constexpr int RB = D * sizeof(T), NF = RB / 64, KT = wt_tiles<T, D>(), KEYS = 16 * KT;
-  constexpr int CPR = RB / 16, NL = kWtRows * CPR / kWtThreads;         // pieces of a row, loads per thread and turn
+  constexpr int CPR = RB / 16, NL = kWtRows * CPR / kWtBlockThreads;    // pieces of a row, loads per thread and turn
   constexpr int LD = RB + 16;
   __shared__ __attribute__((aligned(16))) unsigned char rows_lds[2][kWtRows * LD];
   __shared__ __attribute__((aligned(16))) float ref_lds[2][kWtRows];
   __shared__ __attribute__((aligned(16))) int last_lds[2][kWtRows];
 
   const int b = blockIdx.z, h = blockIdx.y, G = a.Hq / a.Hkv, tid = threadIdx.x;
-  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, grp = lane >> 4;
+  const int lane = tid & 63, l16 = lane & 15, grp = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6) % kWtWaves, group = __builtin_amdgcn_readfirstlane(tid >> 6) / kWtWaves;
   const ChunkExtent e = chunk_extent(a.r, a.c, b);
   const int kfirst = blockIdx.x * kWtWaves * KEYS;       // of the workgroup
   if (kfirst >= e.len) return;                           // workgroup-uniform
@@ -259,7 +262,7 @@ __global__ __launch_bounds__(kWtThreads, 2) void weights_block_kernel(WeightsArg
   auto fetch = [&](int r0) __attribute__((always_inline)) {
 #pragma unroll
     for (int x = 0; x < NL; ++x) {
-      const int c = tid + kWtThreads * x, row = min(r0 + c / CPR, rows - 1);
+      const int c = tid + kWtBlockThreads * x, row = min(r0 + c / CPR, rows - 1);
       const int i = row / G, hq = h * G + row - i * G;
       next[x] = *reinterpret_cast<const u32x4*>(static_cast<const char*>(a.Q) + ((size_t)(e.row0 + i) * a.Hq + hq) * RB + 16 * (c % CPR));
     }
@@ -273,7 +276,7 @@ __global__ __launch_bounds__(kWtThreads, 2) void weights_block_kernel(WeightsArg
   auto place = [&](int buf) __attribute__((always_inline)) {
 #pragma unroll
     for (int x = 0; x < NL; ++x) {
-      const int c = tid + kWtThreads * x;
+      const int c = tid + kWtBlockThreads * x;
       *reinterpret_cast<u32x4*>(rows_lds[buf] + (c / CPR) * LD + 16 * (c % CPR)) = next[x];
     }
     if (tid < kWtRows) {
@@ -291,7 +294,8 @@ __global__ __launch_bounds__(kWtThreads, 2) void weights_block_kernel(WeightsArg
     if (r0 + kWtRows < rows) fetch(r0 + kWtRows);
     const bool masked = ctx + r0 / G < kbase + KEYS - 1;
 #pragma unroll
-    for (int rt = 0; rt < kWtRows / 16; ++rt) {
+    for (int r16 = 0; r16 < kWtRows / 16 / kWtGroups; ++r16) {
+      const int rt = group * (kWtRows / 16 / kWtGroups) + r16;
       frag q[NF];
 #pragma unroll
       for (int f = 0; f < NF; ++f) q[f] = *reinterpret_cast<const frag*>(rows_lds[buf] + (16 * rt + l16) * LD + 64 * f + 16 * grp);
@@ -307,11 +311,18 @@ __global__ __launch_bounds__(kWtThreads, 2) void weights_block_kernel(WeightsArg
     if (r0 + kWtRows < rows) place(buf ^ 1);             // read by nobody since the barrier before
     __syncthreads();
   }
+  // the second group's sums to the first (the rows' area is free behind the last barrier)
+  float* sm = reinterpret_cast<float*>(rows_lds) + wave * KEYS;
 #pragma unroll
   for (int kt = 0; kt < KT; ++kt) {
     sum[kt] = groups_sum(sum[kt]);
-    if (grp == 0 && kbase + 16 * kt + l16 < e.len) a.c.W[home[kt]] = sum[kt] + (a.W_in ? a.decay * a.W_in[home[kt]] : 0.f);
+    if (group == 1 && grp == 0) sm[16 * kt + l16] = sum[kt];
   }
+  __syncthreads();
+  if (group == 1 || grp != 0) return;
+#pragma unroll
+  for (int kt = 0; kt < KT; ++kt)
+    if (kbase + 16 * kt + l16 < e.len) a.c.W[home[kt]] = sum[kt] + sm[16 * kt + l16] + (a.W_in ? a.decay * a.W_in[home[kt]] : 0.f);
 }
 
 template <typename T, int D>
@@ -400,7 +411,7 @@ hipError_t launch(WeightsArgs a, hipStream_t s) {
   }
   constexpr int KEYS = 16 * wt_tiles<T, D>();
   const int blocks = (a.c.cap + KEYS * kWtWaves - 1) / (KEYS * kWtWaves);
-  if ((long long)blocks * a.Hkv * a.r.B >= 256) hipLaunchKernelGGL((weights_block_kernel<T, D>), dim3(blocks, a.Hkv, a.r.B), threads, 0, s, a);
+  if ((long long)blocks * a.Hkv * a.r.B >= 256) hipLaunchKernelGGL((weights_block_kernel<T, D>), dim3(blocks, a.Hkv, a.r.B), dim3(kWtBlockThreads), 0, s, a);
   else hipLaunchKernelGGL((weights_share_kernel<T, D>), dim3((a.c.cap + KEYS - 1) / KEYS, a.Hkv, a.r.B), threads, 0, s, a);
   return hipGetLastError();
 }
