@@ -139,14 +139,14 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(EvictArgs a) 
   }
 }
 
-// blockIdx: x: part of the work, y: KV head, z: request.  IN_ORDER: x = 0 .. 2 * parts - 1 are the column parts of K and V, 2 * parts the
-// weights; otherwise x takes a share of the rows with everything that belongs to them.
+// blockIdx: x: KV head (the heads of a token lie side by side), y: part of the work, z: request.  IN_ORDER: y = 0 .. 2 * parts - 1 are the
+// column parts of K and V, 2 * parts the weights; otherwise y takes a share of the rows with everything that belongs to them.
 template <bool IN_ORDER>
 __global__ __launch_bounds__(IN_ORDER ? 1024 : kMoveThreads) void evict_move_kernel(EvictArgs a, int parts) {
   typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
-  const int h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
+  const int h = blockIdx.x, part = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
   const int n = min(max(a.src.lens[b], 0), a.src.cap), m = min(min(n, a.budget), a.dst.cap);
-  if (blockIdx.x == 0 && h == 0 && tid == 0) a.lens_out[b] = m;
+  if (part == 0 && h == 0 && tid == 0) a.lens_out[b] = m;
   const int* kept = a.kept + ((size_t)b * a.Hkv + h) * a.budget;
   const int s_slots = (1 << a.src.shift) - 1, d_slots = (1 << a.dst.shift) - 1;
   auto from = [&](int j) __attribute__((always_inline)) -> size_t { return ((((size_t)page_of(a.src, b, j)) << a.src.shift) + (j & s_slots)) * a.Hkv + h; };
@@ -155,7 +155,7 @@ __global__ __launch_bounds__(IN_ORDER ? 1024 : kMoveThreads) void evict_move_ker
   auto w_to = [&](int k) __attribute__((always_inline)) -> size_t { return (((size_t)page_of(a.dst, b, k) * a.Hkv + h) << a.dst.shift) + (k & d_slots); };
   if (IN_ORDER) {
     constexpr int NT = 1024;
-    if ((int)blockIdx.x == 2 * parts) {
+    if (part == 2 * parts) {
       for (int k0 = 0; k0 < m; k0 += NT) {
         const int k = k0 + tid;
         const float w = k < m ? a.src.W[w_from(kept[k])] : 0.f;
@@ -166,10 +166,10 @@ __global__ __launch_bounds__(IN_ORDER ? 1024 : kMoveThreads) void evict_move_ker
     }
     const int pieces = a.row_bytes / 16 / parts;          // 16-byte pieces of a row that this workgroup moves
     const int rows = NT / pieces;
-    const bool is_v = (int)blockIdx.x >= parts;
+    const bool is_v = part >= parts;
     const char* src = static_cast<const char*>(is_v ? a.src.V : a.src.K);
     char* dst = static_cast<char*>(is_v ? a.dst.V : a.dst.K);
-    const size_t off = 16 * ((blockIdx.x % parts) * pieces + tid % pieces);
+    const size_t off = 16 * ((part % parts) * pieces + tid % pieces);
     for (int k0 = 0; k0 < m; k0 += rows) {
       const int k = k0 + tid / pieces;
       u32x4 v = {0, 0, 0, 0};
@@ -181,7 +181,7 @@ __global__ __launch_bounds__(IN_ORDER ? 1024 : kMoveThreads) void evict_move_ker
     constexpr int U = kMoveRows;
     const int pieces = a.row_bytes / 16, rows = kMoveThreads / pieces;
     const size_t off = 16 * (tid % pieces);
-    for (int k0 = blockIdx.x * rows * U + tid / pieces; k0 < m; k0 += gridDim.x * rows * U) {
+    for (int k0 = part * rows * U + tid / pieces; k0 < m; k0 += gridDim.y * rows * U) {
       u32x4 x[U], y[U];
       int j[U];
       size_t d[U];
@@ -203,7 +203,7 @@ __global__ __launch_bounds__(IN_ORDER ? 1024 : kMoveThreads) void evict_move_ker
         }
     }
     // the weights, one per thread
-    for (int k = blockIdx.x * kMoveThreads + tid; k < m; k += gridDim.x * kMoveThreads) a.dst.W[w_to(k)] = a.src.W[w_from(kept[k])];
+    for (int k = part * kMoveThreads + tid; k < m; k += gridDim.y * kMoveThreads) a.dst.W[w_to(k)] = a.src.W[w_from(kept[k])];
   }
 }
 
@@ -218,11 +218,11 @@ hipError_t launch_evict(const EvictArgs& a, hipStream_t s) {
   if ((e = hipGetLastError()) != hipSuccess) return e;
   if (a.dst.K == a.src.K) {
     const int parts = a.row_bytes / 64;                   // pieces of 64 bytes
-    hipLaunchKernelGGL((evict_move_kernel<true>), dim3(2 * parts + 1, a.Hkv, a.B), dim3(1024), 0, s, a, parts);
+    hipLaunchKernelGGL((evict_move_kernel<true>), dim3(a.Hkv, 2 * parts + 1, a.B), dim3(1024), 0, s, a, parts);
   } else {
     const int rows = kMoveThreads / (a.row_bytes / 16) * kMoveRows, most_rows = std::min(a.budget, a.src.cap);
     const int share = std::max(1, std::min((most_rows + rows - 1) / rows, 4096 / std::max(1, a.Hkv * a.B)));
-    hipLaunchKernelGGL((evict_move_kernel<false>), dim3(share, a.Hkv, a.B), dim3(kMoveThreads), 0, s, a, 1);
+    hipLaunchKernelGGL((evict_move_kernel<false>), dim3(a.Hkv, share, a.B), dim3(kMoveThreads), 0, s, a, 1);
   }
   return hipGetLastError();
 }

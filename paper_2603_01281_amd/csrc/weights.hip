@@ -15,6 +15,7 @@
 // nothing to hide its latencies behind: a chunk of 1000 over 8192, 32 / 8 heads, 142 us).  weights_share_kernel, where those would leave compute units idle: 64 keys per workgroup,
 // every wave its share of the rows, straight from the caches; the waves' sums are joined in LDS.
 #include <algorithm>
+#include <type_traits>
 
 #include "paged.h"
 
@@ -26,7 +27,9 @@ constexpr int kWtWaves = 4, kWtThreads = 64 * kWtWaves;
 // tiles of 16 keys that a wave holds (four of fp32 rows of 512 bytes did not fit its registers)
 template <typename T, int D> constexpr int wt_tiles() { return D * sizeof(T) > 256 ? 2 : 4; }
 constexpr int kWtRows = 64;                     // rows that pass through LDS at a time
-constexpr int kWtGroups = 2, kWtBlockThreads = kWtThreads * kWtGroups;      // of waves with the same keys, each with its share of those rows
+constexpr int kWtGroups = 2, kWtBlockWaves = 8;     // groups of waves with the same keys, each with its share of those rows; waves of a group
+constexpr int kWtBlockThreads = 64 * kWtGroups * kWtBlockWaves;
+template <typename T, int D> constexpr int wt_block_tiles() { return wt_tiles<T, D>() / 2; }      // 128 registers: four waves to a SIMD
 
 template <typename T> struct WtMath;
 template <> struct WtMath<uint16_t> {
@@ -63,6 +66,37 @@ __device__ __forceinline__ f32x4 wt_tile(const typename WtMath<T>::frag (&q)[NF]
 
 // A row's log-sum-exp in units of the exponent; rows that saw nothing count nothing: exp(. - inf) = 0.
 __device__ __forceinline__ float wt_reference(float lse) { return lse == -INFINITY ? INFINITY : lse * 1.4426950408889634f; }
+
+// One tile of rows against the wave's keys: all products, then all exponentials, so that one key tile's hide behind another's.
+template <bool MASKED, typename T, int NF, int KT>
+__device__ __forceinline__ void wt_rows(const typename WtMath<T>::frag (&q)[NF], const typename WtMath<T>::frag (&kf)[KT][NF], const float (&ref)[4],
+                                        const int (&last)[4], int kbase, float c2, float (&sum)[KT]) {
+  const int l16 = threadIdx.x & 15;
+  f32x4 s[KT];
+#pragma unroll
+  for (int kt = 0; kt < KT; ++kt) s[kt] = wt_tile<T, NF>(q, kf[kt]);
+#pragma unroll
+  for (int kt = 0; kt < KT; ++kt) {
+    float p[4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) p[x] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][x], c2, -ref[x]));
+    if (MASKED) {
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+        if (kbase + 16 * kt + l16 > last[x]) p[x] = 0.f;
+    }
+    sum[kt] += (p[0] + p[1]) + (p[2] + p[3]);
+  }
+}
+
+// The keys have arrived: a wait for them inside the loop over the rows would wait for the next rows too.
+template <int KT, int NF, typename F>
+__device__ __forceinline__ void wt_arrived(F (&kf)[KT][NF]) {
+#pragma unroll
+  for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+    for (int f = 0; f < NF; ++f) asm volatile("" : "+v"(kf[kt][f]));
+}
 
 // ---- few rows ------------------------------------------------------------------------------------------------------------
 
@@ -161,28 +195,21 @@ __global__ __launch_bounds__(kRowWaves * 64, 2) void weights_stream_kernel(Weigh
     home = home_next;
     if (kb + kRowWaves * BK < k1) fetch(kb + kRowWaves * BK);
     float sum[KT];
-    const bool masked = kb + BK - 1 > all_see;
+    frag k[KT][NF];
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt) {
-      frag k[NF];
-#pragma unroll
-      for (int f = 0; f < NF; ++f) k[f] = *reinterpret_cast<const frag*>(tile + (16 * kt + l16) * LD + 64 * f + 16 * grp);
       sum[kt] = 0.f;
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
-        const f32x4 s = wt_tile<T, NF>(q[rt], k);
-        float p[4];
-#pragma unroll
-        for (int x = 0; x < 4; ++x) p[x] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x], c2, -ref[rt][x]));
-        if (masked) {
-#pragma unroll
-          for (int x = 0; x < 4; ++x)
-            if (kb + 16 * kt + l16 > last[rt][x]) p[x] = 0.f;
-        }
-        sum[kt] += (p[0] + p[1]) + (p[2] + p[3]);
-      }
-      sum[kt] = groups_sum(sum[kt]);
+      for (int f = 0; f < NF; ++f) k[kt][f] = *reinterpret_cast<const frag*>(tile + (16 * kt + l16) * LD + 64 * f + 16 * grp);
     }
+    const bool masked = kb + BK - 1 > all_see;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      if (masked) wt_rows<true, T, NF, KT>(q[rt], k, ref[rt], last[rt], kb, c2, sum);
+      else wt_rows<false, T, NF, KT>(q[rt], k, ref[rt], last[rt], kb, c2, sum);
+    }
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt) sum[kt] = groups_sum(sum[kt]);
     asm volatile("" ::: "memory");         // the tile is rewritten behind these reads
     if (lane < BK && kb + lane < k1) a.c.W[home] = (KT == 2 && grp == 1 ? sum[KT - 1] : sum[0]) + (a.W_in ? a.decay * w : 0.f);
   }
@@ -206,31 +233,11 @@ __device__ __forceinline__ void wt_keys(const WeightsArgs& a, const ChunkExtent&
   }
 }
 
-// One tile of rows against the wave's keys.
-template <typename T, int NF, int KT>
-__device__ __forceinline__ void wt_rows(const typename WtMath<T>::frag (&q)[NF], const typename WtMath<T>::frag (&kf)[KT][NF], const float (&ref)[4],
-                                        const int (&last)[4], bool masked, int kbase, float c2, float (&sum)[KT]) {
-  const int l16 = threadIdx.x & 15;
-#pragma unroll
-  for (int kt = 0; kt < KT; ++kt) {
-    const f32x4 s = wt_tile<T, NF>(q, kf[kt]);
-    float p[4];
-#pragma unroll
-    for (int x = 0; x < 4; ++x) p[x] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x], c2, -ref[x]));
-    if (masked) {
-#pragma unroll
-      for (int x = 0; x < 4; ++x)
-        if (kbase + 16 * kt + l16 > last[x]) p[x] = 0.f;
-    }
-    sum[kt] += (p[0] + p[1]) + (p[2] + p[3]);
-  }
-}
-
 template <typename T, int D>
-__global__ __launch_bounds__(kWtBlockThreads, 2) void weights_block_kernel(WeightsArgs a) {
+__global__ __launch_bounds__(kWtBlockThreads, 4) void weights_block_kernel(WeightsArgs a) {
   typedef typename WtMath<T>::frag frag;
-  constexpr int RB = D * sizeof(T), NF = RB / 64, KT = wt_tiles<T, D>(), KEYS = 16 * KT;
-  constexpr int CPR = RB / 16, NL = kWtRows * CPR / kWtBlockThreads;    // pieces of a row, loads per thread and turn
+  constexpr int RB = D * sizeof(T), NF = RB / 64, KT = wt_block_tiles<T, D>(), KEYS = 16 * KT;
+  constexpr int CPR = RB / 16, NL = (kWtRows * CPR + kWtBlockThreads - 1) / kWtBlockThreads;    // pieces of a row, loads per thread and turn
   constexpr int LD = RB + 16;
   __shared__ __attribute__((aligned(16))) unsigned char rows_lds[2][kWtRows * LD];
   __shared__ __attribute__((aligned(16))) float ref_lds[2][kWtRows];
@@ -238,9 +245,9 @@ __global__ __launch_bounds__(kWtBlockThreads, 2) void weights_block_kernel(Weigh
 
   const int b = blockIdx.z, h = blockIdx.y, G = a.Hq / a.Hkv, tid = threadIdx.x;
   const int lane = tid & 63, l16 = lane & 15, grp = lane >> 4;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6) % kWtWaves, group = __builtin_amdgcn_readfirstlane(tid >> 6) / kWtWaves;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6) % kWtBlockWaves, group = __builtin_amdgcn_readfirstlane(tid >> 6) / kWtBlockWaves;
   const ChunkExtent e = chunk_extent(a.r, a.c, b);
-  const int kfirst = blockIdx.x * kWtWaves * KEYS;       // of the workgroup
+  const int kfirst = blockIdx.x * kWtBlockWaves * KEYS;       // of the workgroup
   if (kfirst >= e.len) return;                           // workgroup-uniform
   const int kbase = kfirst + wave * KEYS;
   frag kf[KT][NF];
@@ -262,7 +269,7 @@ __global__ __launch_bounds__(kWtBlockThreads, 2) void weights_block_kernel(Weigh
   auto fetch = [&](int r0) __attribute__((always_inline)) {
 #pragma unroll
     for (int x = 0; x < NL; ++x) {
-      const int c = tid + kWtBlockThreads * x, row = min(r0 + c / CPR, rows - 1);
+      const int c = tid + kWtBlockThreads * x, row = min(r0 + min(c / CPR, kWtRows - 1), rows - 1);
       const int i = row / G, hq = h * G + row - i * G;
       next[x] = *reinterpret_cast<const u32x4*>(static_cast<const char*>(a.Q) + ((size_t)(e.row0 + i) * a.Hq + hq) * RB + 16 * (c % CPR));
     }
@@ -277,7 +284,7 @@ __global__ __launch_bounds__(kWtBlockThreads, 2) void weights_block_kernel(Weigh
 #pragma unroll
     for (int x = 0; x < NL; ++x) {
       const int c = tid + kWtBlockThreads * x;
-      *reinterpret_cast<u32x4*>(rows_lds[buf] + (c / CPR) * LD + 16 * (c % CPR)) = next[x];
+      if (kWtRows * CPR % kWtBlockThreads == 0 || c < kWtRows * CPR) *reinterpret_cast<u32x4*>(rows_lds[buf] + (c / CPR) * LD + 16 * (c % CPR)) = next[x];
     }
     if (tid < kWtRows) {
       ref_lds[buf][tid] = ref_next;
@@ -288,26 +295,30 @@ __global__ __launch_bounds__(kWtBlockThreads, 2) void weights_block_kernel(Weigh
     fetch(r_lo);
     place(0);
   }
+  wt_arrived(kf);
   __syncthreads();
   int buf = 0;
   for (int r0 = r_lo; r0 < rows; r0 += kWtRows, buf ^= 1) {
     if (r0 + kWtRows < rows) fetch(r0 + kWtRows);
-    const bool masked = ctx + r0 / G < kbase + KEYS - 1;
+    auto turn = [&](auto masked) __attribute__((always_inline)) {
 #pragma unroll
-    for (int r16 = 0; r16 < kWtRows / 16 / kWtGroups; ++r16) {
-      const int rt = group * (kWtRows / 16 / kWtGroups) + r16;
-      frag q[NF];
+      for (int r16 = 0; r16 < kWtRows / 16 / kWtGroups; ++r16) {
+        const int rt = group * (kWtRows / 16 / kWtGroups) + r16;
+        frag q[NF];
 #pragma unroll
-      for (int f = 0; f < NF; ++f) q[f] = *reinterpret_cast<const frag*>(rows_lds[buf] + (16 * rt + l16) * LD + 64 * f + 16 * grp);
-      float ref[4];
-      int last[4];
+        for (int f = 0; f < NF; ++f) q[f] = *reinterpret_cast<const frag*>(rows_lds[buf] + (16 * rt + l16) * LD + 64 * f + 16 * grp);
+        float ref[4];
+        int last[4];
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        ref[x] = ref_lds[buf][16 * rt + 4 * grp + x];
-        last[x] = last_lds[buf][16 * rt + 4 * grp + x];
+        for (int x = 0; x < 4; ++x) {
+          ref[x] = ref_lds[buf][16 * rt + 4 * grp + x];
+          last[x] = decltype(masked)::value ? last_lds[buf][16 * rt + 4 * grp + x] : 0;
+        }
+        wt_rows<decltype(masked)::value, T, NF, KT>(q, kf, ref, last, kbase, c2, sum);
       }
-      wt_rows<T, NF, KT>(q, kf, ref, last, masked, kbase, c2, sum);
-    }
+    };
+    if (ctx + r0 / G < kbase + KEYS - 1) turn(std::true_type{});
+    else turn(std::false_type{});
     if (r0 + kWtRows < rows) place(buf ^ 1);             // read by nobody since the barrier before
     __syncthreads();
   }
@@ -359,6 +370,7 @@ __global__ __launch_bounds__(kWtThreads, 2) void weights_share_kernel(WeightsArg
     i_n = i;
   };
   int r0 = r_lo + 16 * wave;
+  wt_arrived(kf);
   if (r0 < rows) fetch(r0);
   for (; r0 < rows; r0 += 16 * kWtWaves) {
     frag q[NF];
@@ -372,7 +384,8 @@ __global__ __launch_bounds__(kWtThreads, 2) void weights_share_kernel(WeightsArg
       last[x] = ctx + __shfl(i_n, 4 * grp + x);
     }
     if (r0 + 16 * kWtWaves < rows) fetch(r0 + 16 * kWtWaves);
-    wt_rows<T, NF, KT>(q, kf, ref, last, ctx + r0 / G < kbase + KEYS - 1, kbase, c2, sum);
+    if (ctx + r0 / G < kbase + KEYS - 1) wt_rows<true, T, NF, KT>(q, kf, ref, last, kbase, c2, sum);
+    else wt_rows<false, T, NF, KT>(q, kf, ref, last, kbase, c2, sum);
   }
 #pragma unroll
   for (int kt = 0; kt < KT; ++kt) {
@@ -410,7 +423,8 @@ hipError_t launch(WeightsArgs a, hipStream_t s) {
     return hipGetLastError();
   }
   constexpr int KEYS = 16 * wt_tiles<T, D>();
-  const int blocks = (a.c.cap + KEYS * kWtWaves - 1) / (KEYS * kWtWaves);
+  constexpr int kBlock = 16 * wt_block_tiles<T, D>() * kWtBlockWaves;
+  const int blocks = (a.c.cap + kBlock - 1) / kBlock;
   if ((long long)blocks * a.Hkv * a.r.B >= 256) hipLaunchKernelGGL((weights_block_kernel<T, D>), dim3(blocks, a.Hkv, a.r.B), dim3(kWtBlockThreads), 0, s, a);
   else hipLaunchKernelGGL((weights_share_kernel<T, D>), dim3((a.c.cap + KEYS - 1) / KEYS, a.Hkv, a.r.B), threads, 0, s, a);
   return hipGetLastError();
