@@ -10,7 +10,7 @@
 // Few rows (generation): HBM-bound, every key is read once.  weights_stream_kernel holds the rows and streams the keys as whole rows
 // through a wave-private LDS tile, a block ahead, over ranges that are cut as for the attention itself (paged.h, plan_item).
 // Many rows: bound by the vector unit (an exponential takes it four times as long as a multiplication; 96 cycles per tile of 16 x 16
-// against 64 of the matrix pipe at D = 128).  weights_block_kernel holds 64 keys per wave in registers and passes the rows by, 64 at a
+// against 64 of the matrix pipe at D = 128).  weights_block_kernel holds 64 keys per wave in registers and passes the rows by, 64 or 128 at a
 // time through LDS for all its waves; two groups of four waves have the same keys and take half of the rows each (one wave per SIMD had
 // nothing to hide its latencies behind: a chunk of 1000 over 8192, 32 / 8 heads, 142 us).  weights_share_kernel, where those would leave compute units idle: 64 keys per workgroup,
 // every wave its share of the rows, straight from the caches; the waves' sums are joined in LDS.
@@ -26,7 +26,7 @@ typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 constexpr int kWtWaves = 4, kWtThreads = 64 * kWtWaves;
 // tiles of 16 keys that a wave holds (four of fp32 rows of 512 bytes did not fit its registers)
 template <typename T, int D> constexpr int wt_tiles() { return D * sizeof(T) > 256 ? 2 : 4; }
-constexpr int kWtRows = 64;                     // rows that pass through LDS at a time
+template <typename T, int D> constexpr int wt_block_rows() { return D * sizeof(T) > 256 ? 64 : 128; }      // rows that pass through LDS at a time
 constexpr int kWtGroups = 2, kWtBlockWaves = 8;     // groups of waves with the same keys, each with its share of those rows; waves of a group
 constexpr int kWtBlockThreads = 64 * kWtGroups * kWtBlockWaves;
 template <typename T, int D> constexpr int wt_block_tiles() { return wt_tiles<T, D>() / 2; }      // 128 registers: four waves to a SIMD
@@ -236,7 +236,7 @@ __device__ __forceinline__ void wt_keys(const WeightsArgs& a, const ChunkExtent&
 template <typename T, int D>
 __global__ __launch_bounds__(kWtBlockThreads, 4) void weights_block_kernel(WeightsArgs a) {
   typedef typename WtMath<T>::frag frag;
-  constexpr int RB = D * sizeof(T), NF = RB / 64, KT = wt_block_tiles<T, D>(), KEYS = 16 * KT;
+  constexpr int RB = D * sizeof(T), NF = RB / 64, KT = wt_block_tiles<T, D>(), KEYS = 16 * KT, kWtRows = wt_block_rows<T, D>();
   constexpr int CPR = RB / 16, NL = (kWtRows * CPR + kWtBlockThreads - 1) / kWtBlockThreads;    // pieces of a row, loads per thread and turn
   constexpr int LD = RB + 16;
   __shared__ __attribute__((aligned(16))) unsigned char rows_lds[2][kWtRows * LD];
@@ -301,20 +301,27 @@ __global__ __launch_bounds__(kWtBlockThreads, 4) void weights_block_kernel(Weigh
   for (int r0 = r_lo; r0 < rows; r0 += kWtRows, buf ^= 1) {
     if (r0 + kWtRows < rows) fetch(r0 + kWtRows);
     auto turn = [&](auto masked) __attribute__((always_inline)) {
+      constexpr int NT = kWtRows / 16 / kWtGroups;       // this group's tiles of the rows
+      const int rt0 = group * NT;
+      constexpr int AHEAD = sizeof(T) == 2;              // a tile's rows are read while the one before is worked on (fp32: no registers left)
+      frag q[1 + AHEAD][NF];
+      auto read = [&](int r16) __attribute__((always_inline)) {
 #pragma unroll
-      for (int r16 = 0; r16 < kWtRows / 16 / kWtGroups; ++r16) {
-        const int rt = group * (kWtRows / 16 / kWtGroups) + r16;
-        frag q[NF];
+        for (int f = 0; f < NF; ++f) q[r16 & AHEAD][f] = *reinterpret_cast<const frag*>(rows_lds[buf] + (16 * (rt0 + r16) + l16) * LD + 64 * f + 16 * grp);
+      };
+      if (AHEAD) read(0);
 #pragma unroll
-        for (int f = 0; f < NF; ++f) q[f] = *reinterpret_cast<const frag*>(rows_lds[buf] + (16 * rt + l16) * LD + 64 * f + 16 * grp);
+      for (int r16 = 0; r16 < NT; ++r16) {
+        if (r16 + AHEAD < NT) read(r16 + AHEAD);
+        const f32x4 ref4 = *reinterpret_cast<const f32x4*>(&ref_lds[buf][16 * (rt0 + r16) + 4 * grp]);
         float ref[4];
         int last[4];
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
-          ref[x] = ref_lds[buf][16 * rt + 4 * grp + x];
-          last[x] = decltype(masked)::value ? last_lds[buf][16 * rt + 4 * grp + x] : 0;
+          ref[x] = ref4[x];
+          last[x] = decltype(masked)::value ? last_lds[buf][16 * (rt0 + r16) + 4 * grp + x] : 0;
         }
-        wt_rows<decltype(masked)::value, T, NF, KT>(q, kf, ref, last, kbase, c2, sum);
+        wt_rows<decltype(masked)::value, T, NF, KT>(q[r16 & AHEAD], kf, ref, last, kbase, c2, sum);
       }
     };
     if (ctx + r0 / G < kbase + KEYS - 1) turn(std::true_type{});
