@@ -85,18 +85,21 @@ def chunk_attention(Q, K, V, table, lens, cu, scale=None):
     for b in range(len(lens)):
         k, v = cached(K, table, b, lens[b]), cached(V, table, b, lens[b])
         n = cu[b + 1] - cu[b]
-        for i in range(n):
-            seen = lens[b] - n + i + 1
-            if seen <= 0:
-                continue
-            for hq in range(Hq):
-                q, h, t = Q[cu[b] + i, hq], hq // G, cu[b] + i
-                s = scale * (k[:seen, h] @ q)
-                p = np.exp(s - s.max())
-                L[hq, t] = s.max() + math.log(p.sum())
-                p /= p.sum()
-                O[t, hq], spread[t, hq] = p @ v[:seen, h], p @ np.abs(v[:seen, h])
-                size[hq, t] = scale * (np.abs(k[:seen, h]) @ np.abs(q)).max()
+        first = max(0, n - lens[b])                        # new tokens before it see nothing
+        if first >= n:
+            continue
+        rows = slice(cu[b] + first, cu[b] + n)
+        hidden = np.arange(lens[b])[None] > (lens[b] - n + np.arange(first, n))[:, None]
+        for hq in range(Hq):
+            h = hq // G
+            s = np.where(hidden, -np.inf, scale * (Q[rows, hq] @ k[:, h].T))
+            top = s.max(1, keepdims=True)
+            p = np.exp(s - top)
+            total_p = p.sum(1, keepdims=True)
+            L[hq, rows] = (top + np.log(total_p))[:, 0]
+            p /= total_p
+            O[rows, hq], spread[rows, hq] = p @ v[:, h], p @ np.abs(v[:, h])
+            size[hq, rows] = np.where(hidden, 0.0, scale * (np.abs(Q[rows, hq]) @ np.abs(k[:, h]).T)).max(1)
     return O, L, spread, size
 
 
@@ -111,11 +114,12 @@ def attention_weights(Q, L, K, W_out, W_in, table, lens, cu, window, decay, scal
         k = cached(K, table, b, lens[b])
         n = cu[b + 1] - cu[b]
         got = np.zeros((lens[b], Hkv))
-        for i in range(max(0, n - window), n):
-            seen = lens[b] - n + i + 1
-            for hq in range(Hq):
-                if seen > 0 and L[hq, cu[b] + i] > -np.inf:
-                    got[:seen, hq // G] += np.exp(scale * (k[:seen, hq // G] @ Q[cu[b] + i, hq]) - L[hq, cu[b] + i])
+        first = max(0, n - window)
+        hidden = np.arange(lens[b])[None] > (lens[b] - n + np.arange(first, n))[:, None]
+        for hq in range(Hq):
+            lse = L[hq, cu[b] + first:cu[b] + n, None]
+            s = scale * (Q[cu[b] + first:cu[b] + n, hq] @ k[:, hq // G].T)
+            got[:, hq // G] += np.where(hidden | np.isneginf(lse), 0.0, np.exp(s - np.where(np.isneginf(lse), 0.0, lse))).sum(0)
         for j in range(lens[b]):
             page, slot = table[b, j // ps], j % ps
             sums[page, :, slot] = got[j]

@@ -20,8 +20,8 @@ namespace {
 typedef __attribute__((address_space(3))) s16x4* row_lds_s16x4_ptr;
 typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
 
-template <int D, int RT>
-__global__ __launch_bounds__(kRowThreads, RT == 4 && D == 128 ? 1 : 2) void chunk_rows_bf16_kernel(ChunkArgs a) {
+template <int D, int RT, int NW>
+__global__ __launch_bounds__(64 * NW, RT == 4 && D == 128 ? 1 : 2) void chunk_rows_bf16_kernel(ChunkArgs a) {
   constexpr int BK = 32, R = 16 * RT;
   // LDS row strides (elements): 16 rows of K at one 16-byte column, and 16 rows x 32 bytes of V, spread over all banks
   constexpr int LDK = D + 8, LDV = D + 16, OLD = D + 4;
@@ -29,8 +29,8 @@ __global__ __launch_bounds__(kRowThreads, RT == 4 && D == 128 ? 1 : 2) void chun
   constexpr int CPR = D / 8, RPI = 64 / CPR, NV = BK / RPI;     // 16-byte pieces per row, rows per load, loads per block
   constexpr int kTileBytes = BK * LDV * 2, kMergeBytes = 16 * OLD * 4;
   constexpr int kAreaBytes = kTileBytes > kMergeBytes ? kTileBytes : kMergeBytes;
-  __shared__ __attribute__((aligned(16))) unsigned char smem[kRowWaves * kAreaBytes];
-  __shared__ float sm_ml[kRowWaves][16][2];
+  __shared__ __attribute__((aligned(16))) unsigned char smem[NW * kAreaBytes];
+  __shared__ float sm_ml[NW][16][2];
 
   ChunkItem it;
   const bool exists = plan_item(a.r, a.c, a.p, blockIdx.x, it);
@@ -79,7 +79,7 @@ __global__ __launch_bounds__(kRowThreads, RT == 4 && D == 128 ? 1 : 2) void chun
   const char* Vh = static_cast<const char*>(a.c.V) + (size_t)h * D * 2;
   const int slots = (1 << a.c.shift) - 1;
   u32x4 kr[NV], vr[NV];
-  PageWindow<BK> win;
+  PageWindow<BK, NW> win;
   int block = 0;                           // of the window
   auto fetch = [&](auto nt, int kb) __attribute__((always_inline)) {
     constexpr bool NT = decltype(nt)::value;
@@ -115,7 +115,7 @@ __global__ __launch_bounds__(kRowThreads, RT == 4 && D == 128 ? 1 : 2) void chun
     win.load(a.c, it.b, kb, k1);
     fetch(nt, kb);
   }
-  for (; kb < k1; kb += kRowWaves * BK) {
+  for (; kb < k1; kb += NW * BK) {
     // (a wave's LDS operations execute in program order; the fences are for the compiler)
 #pragma unroll
     for (int x = 0; x < NV; ++x) *reinterpret_cast<u32x4*>(tile + (RPI * x + lane / CPR) * LDK + 8 * (lane % CPR)) = kr[x];
@@ -137,7 +137,7 @@ __global__ __launch_bounds__(kRowThreads, RT == 4 && D == 128 ? 1 : 2) void chun
 #pragma unroll
     for (int x = 0; x < NV; ++x) *reinterpret_cast<u32x4*>(tile + (RPI * x + lane / CPR) * LDV + 8 * (lane % CPR)) = vr[x];
     asm volatile("" ::: "memory");
-    const int kb_next = kb + kRowWaves * BK;
+    const int kb_next = kb + NW * BK;
     if (kb_next < k1) fetch(nt, kb_next);      // on their way during the softmax
 
     bf16x8 pb[RT];
@@ -200,44 +200,51 @@ __global__ __launch_bounds__(kRowThreads, RT == 4 && D == 128 ? 1 : 2) void chun
       sm_ml[wave][l16][1] = lt;
     }
     __syncthreads();
-    merge_waves<uint16_t, D>(a, it, h, it.rc * R + 16 * rt, reinterpret_cast<const float*>(smem), sm_ml);
+    merge_waves<uint16_t, D, NW>(a, it, h, it.rc * R + 16 * rt, reinterpret_cast<const float*>(smem), sm_ml);
   }
 }
 
+template <int D, int NW>
+void launch_rows(const ChunkArgs& a, const RowPlan& r, hipStream_t s) {
+  const dim3 grid(r.items, a.Hkv), block(64 * NW);
+  if (r.rows16 == 1) hipLaunchKernelGGL((chunk_rows_bf16_kernel<D, 1, NW>), grid, block, 0, s, a);
+  else if (r.rows16 == 2) hipLaunchKernelGGL((chunk_rows_bf16_kernel<D, 2, NW>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((chunk_rows_bf16_kernel<D, 4, 4>), grid, dim3(256), 0, s, a);
+}
+
 template <int D>
-hipError_t launch_rows(const ChunkArgs& a, int rows16, int items, int rows, hipStream_t s) {
-  const dim3 grid(items, a.Hkv), block(kRowThreads);
-  if (rows16 == 1) hipLaunchKernelGGL((chunk_rows_bf16_kernel<D, 1>), grid, block, 0, s, a);
-  else if (rows16 == 2) hipLaunchKernelGGL((chunk_rows_bf16_kernel<D, 2>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((chunk_rows_bf16_kernel<D, 4>), grid, block, 0, s, a);
-  launch_chunk_merge<uint16_t, D>(a, items, rows, s);
+hipError_t launch_rows(const ChunkArgs& a, const RowPlan& r, hipStream_t s) {
+  if (r.waves == 8) launch_rows<D, 8>(a, r, s);
+  else launch_rows<D, 4>(a, r, s);
+  launch_chunk_merge<uint16_t, D>(a, r.items, r.rows, s);
   return hipGetLastError();
 }
 
 // Rows per workgroup, ranges and the bounds of both, from what the host knows: B requests, `total` new tokens of which no request
 // has more than max_q, caches of up to S tokens.
-struct RowPlan {
-  ChunkPlan p;
-  int rows16, rows, items;               // tiles of 16 rows, rows that a chunk can have, items
-};
 RowPlan row_plan(int B, int S, int Hq, int Hkv, int D, int dtype, int total, int max_q) {
   RowPlan r;
-  const int G = Hq / Hkv;
+  const int G = Hq / Hkv, blocks = (S + 31) / 32;
+  const bool bf16 = dtype == SEKA_BF16;
   const long long rows = (long long)std::min(max_q, total) * G;
   r.rows16 = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
   r.p.R = 16 * r.rows16;
   r.p.G = G;
   r.rows = (int)std::min(rows, (long long)r.p.R);
-  const int chunks = (int)std::min(((long long)total * G) / r.p.R + B, (long long)0x3fffffff);
-  // two workgroups of four waves to a compute unit, about
+  const long long chunks = std::min(((long long)total * G) / r.p.R + B, 0x3fffffffll);
+  // eight waves to a workgroup where the keys are few: a range is then half as long a chain
+  const bool few = r.rows16 <= 2 && chunks * blocks * Hkv <= 256 * 8 * 2;
+  r.waves = few ? 8 : 4;
+  // two workgroups of four waves to a compute unit, about, or one of eight
   r.p.slots_log2 = 0;
-  while ((1 << r.p.slots_log2) * Hkv < 512) ++r.p.slots_log2;
-  r.p.least = 8;                           // 256 tokens
-  r.p.streams = (long long)(300e6 / (2.0 * 32 * Hkv * D * (dtype == SEKA_BF16 ? 2 : 4)));
-  const int blocks = (S + 31) / 32;
+  while ((1 << r.p.slots_log2) * Hkv < (few ? 256 : 512)) ++r.p.slots_log2;
+  r.p.least = bf16 ? 8 : 4;                // 256 tokens, 128: a block of every wave of eight
   r.p.max_splits = std::max(1, std::min(kMaxRanges, (blocks + r.p.least - 1) / r.p.least));
+  // and no second kernel where a wave has no more than four blocks
+  if (few && S <= (bf16 ? 1024 : 512)) r.p.max_splits = 1;
+  r.p.streams = (long long)(300e6 / (2.0 * 32 * Hkv * D * (bf16 ? 2 : 4)));
   // sum over chunks of ceil(blocks / L) <= T / L + chunks with T / L <= slots, and no more than every chunk in all its ranges
-  r.items = (int)std::min((long long)chunks + (1 << r.p.slots_log2), (long long)chunks * r.p.max_splits);
+  r.items = (int)std::min(chunks + (1 << r.p.slots_log2), chunks * r.p.max_splits);
   return r;
 }
 
@@ -251,11 +258,15 @@ int compute_units() {
   });
 }
 
+constexpr double kPipeLeastFlops = 3e9;
+
 // Whether a call's chunks go to the pipelined kernel, and how: bf16, more rows per KV head than four tiles of 16, and a cache
 // whose page numbers fit beside the tiles in LDS (4 bytes for every page of S tokens).
 bool pipe_plan(int S, int Hq, int Hkv, int D, int dtype, int shift, int total, int max_q, PipeChunkPlan* out) {
   const int G = Hq / Hkv;
   if (dtype != SEKA_BF16 || (long long)std::min(max_q, total) * G <= 64) return false;
+  // little work goes to the kernel of few rows all the same: this one takes some 30 us for any
+  if (4.0 * D * total * Hq * S <= kPipeLeastFlops) return false;
   out->hpw = G % 4 == 0 ? 4 : G % 7 == 0 ? 7 : G % 2 == 0 ? 2 : 1;
   out->rbw = out->hpw == 7 ? 1 : 8 / out->hpw;
   const int nHC = Hq / out->hpw, cus = compute_units();
@@ -268,8 +279,8 @@ bool pipe_plan(int S, int Hq, int Hkv, int D, int dtype, int shift, int total, i
 
 }  // namespace
 
-hipError_t launch_chunk_bf16(const ChunkArgs& a, int D, int rows16, int items, int rows, hipStream_t s) {
-  return D == 128 ? launch_rows<128>(a, rows16, items, rows, s) : launch_rows<64>(a, rows16, items, rows, s);
+hipError_t launch_chunk_bf16(const ChunkArgs& a, int D, const RowPlan& r, hipStream_t s) {
+  return D == 128 ? launch_rows<128>(a, r, s) : launch_rows<64>(a, r, s);
 }
 
 size_t row_states(const RowPlan& r, int Hkv, int D) { return r.p.max_splits > 1 ? (size_t)r.items * Hkv * r.p.R * (D + 4) * sizeof(float) : 0; }
@@ -292,7 +303,7 @@ hipError_t launch_chunk(ChunkArgs a, int D, int dtype, int S, hipStream_t s) {
   const RowPlan r = row_plan(a.r.B, S, a.Hq, a.Hkv, D, dtype, a.r.total, a.r.max_q);
   a.p = r.p;
   a.items_of = reinterpret_cast<int4*>(reinterpret_cast<char*>(a.part) + row_states(r, a.Hkv, D));
-  return dtype == SEKA_BF16 ? launch_chunk_bf16(a, D, r.rows16, r.items, r.rows, s) : launch_chunk_f32(a, D, r.rows16, r.items, r.rows, s);
+  return dtype == SEKA_BF16 ? launch_chunk_bf16(a, D, r, s) : launch_chunk_f32(a, D, r, s);
 }
 
 }  // namespace seka

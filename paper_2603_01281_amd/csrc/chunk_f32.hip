@@ -11,13 +11,13 @@
 namespace seka {
 namespace {
 
-template <int D, int RT>
-__global__ __launch_bounds__(kRowThreads, RT == 4 ? 1 : 2) void chunk_rows_f32_kernel(ChunkArgs a) {
+template <int D, int RT, int NW>
+__global__ __launch_bounds__(64 * NW, RT == 4 ? 1 : 2) void chunk_rows_f32_kernel(ChunkArgs a) {
   constexpr int NCH = RT == 1 ? 8 : RT == 2 ? 4 : 2;
   constexpr int KI = D / 16, VH = D / 64, DX = D / 16;
   constexpr int BK = 16, OLD = D + 4, R = 16 * RT;
-  __shared__ __attribute__((aligned(16))) float sm_o[kRowWaves * 16 * OLD];
-  __shared__ float sm_ml[kRowWaves][16][2];
+  __shared__ __attribute__((aligned(16))) float sm_o[NW * 16 * OLD];
+  __shared__ float sm_ml[NW][16][2];
 
   ChunkItem it;
   const bool exists = plan_item(a.r, a.c, a.p, blockIdx.x, it);
@@ -50,7 +50,7 @@ __global__ __launch_bounds__(kRowThreads, RT == 4 ? 1 : 2) void chunk_rows_f32_k
   const float* Kh = static_cast<const float*>(a.c.K) + (size_t)h * D + 4 * g;
   const float* Vh = static_cast<const float*>(a.c.V) + (size_t)h * D + 4 * l16;
   const int slots = (1 << a.c.shift) - 1;
-  PageWindow<BK> win;
+  PageWindow<BK, NW> win;
   int block = 0, at = 0;
   f32x4 kv[KI], vv[4][VH];
   auto turn_window = [&](int kb) __attribute__((always_inline)) {
@@ -89,7 +89,7 @@ __global__ __launch_bounds__(kRowThreads, RT == 4 ? 1 : 2) void chunk_rows_f32_k
     for (int x = 0; x < DX; ++x) o[rt][x] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   const float c2 = a.scale * 1.4426950408889634f;
-  constexpr int TURN = kRowWaves * BK;
+  constexpr int TURN = NW * BK;
   int kb = k0 + wave * BK;
   if (kb < k1) {
     win.load(a.c, it.b, kb, k1);
@@ -168,24 +168,30 @@ __global__ __launch_bounds__(kRowThreads, RT == 4 ? 1 : 2) void chunk_rows_f32_k
       sm_ml[wave][l16][1] = lt;
     }
     __syncthreads();
-    merge_waves<float, D>(a, it, h, it.rc * R + 16 * rt, sm_o, sm_ml);
+    merge_waves<float, D, NW>(a, it, h, it.rc * R + 16 * rt, sm_o, sm_ml);
   }
 }
 
+template <int D, int NW>
+void launch_rows(const ChunkArgs& a, const RowPlan& r, hipStream_t s) {
+  const dim3 grid(r.items, a.Hkv), block(64 * NW);
+  if (r.rows16 == 1) hipLaunchKernelGGL((chunk_rows_f32_kernel<D, 1, NW>), grid, block, 0, s, a);
+  else if (r.rows16 == 2) hipLaunchKernelGGL((chunk_rows_f32_kernel<D, 2, NW>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((chunk_rows_f32_kernel<D, 4, 4>), grid, dim3(256), 0, s, a);
+}
+
 template <int D>
-hipError_t launch_rows(const ChunkArgs& a, int rows16, int items, int rows, hipStream_t s) {
-  const dim3 grid(items, a.Hkv), block(kRowThreads);
-  if (rows16 == 1) hipLaunchKernelGGL((chunk_rows_f32_kernel<D, 1>), grid, block, 0, s, a);
-  else if (rows16 == 2) hipLaunchKernelGGL((chunk_rows_f32_kernel<D, 2>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((chunk_rows_f32_kernel<D, 4>), grid, block, 0, s, a);
-  launch_chunk_merge<float, D>(a, items, rows, s);
+hipError_t launch_rows(const ChunkArgs& a, const RowPlan& r, hipStream_t s) {
+  if (r.waves == 8) launch_rows<D, 8>(a, r, s);
+  else launch_rows<D, 4>(a, r, s);
+  launch_chunk_merge<float, D>(a, r.items, r.rows, s);
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_chunk_f32(const ChunkArgs& a, int D, int rows16, int items, int rows, hipStream_t s) {
-  return D == 128 ? launch_rows<128>(a, rows16, items, rows, s) : launch_rows<64>(a, rows16, items, rows, s);
+hipError_t launch_chunk_f32(const ChunkArgs& a, int D, const RowPlan& r, hipStream_t s) {
+  return D == 128 ? launch_rows<128>(a, r, s) : launch_rows<64>(a, r, s);
 }
 
 }  // namespace seka

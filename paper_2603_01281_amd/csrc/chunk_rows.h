@@ -6,45 +6,52 @@
 
 namespace seka {
 
-constexpr int kRowThreads = 64 * kRowWaves;
 constexpr float kRowSlack = 8.f;         // a row's reference exponent trails its maximum by at most this (base 2)
 constexpr float kRowLow = -1e30f;        // reference of a row that has seen nothing
 
-// Merged state of output column d of a row: the output itself if the item has its rows to itself, else a partial state.
+// Merged state of four output columns of a row: the output itself if the item has its rows to itself, else a partial state.
 template <typename T, int D>
-__device__ __forceinline__ void row_emit(const ChunkArgs& a, const ChunkItem& it, int h, int row, int d, float m, float l, float o) {
-  const int G = a.p.G, i = row / G, hq = h * G + row % G;
-  if (it.splits == 1) {
-    const float v = l > 0.f || l != l ? o / l : 0.f;
-    T* O = static_cast<T*>(a.O) + ((size_t)(it.e.row0 + i) * a.Hq + hq) * D + d;
-    if constexpr (sizeof(T) == 2) *O = __builtin_bit_cast(T, (__bf16)v);
-    else *O = v;
-    if (a.lse && d == 0) a.lse[(size_t)hq * a.r.total + it.e.row0 + i] = l > 0.f || l != l ? m * 0.6931471805599453f + logf(l) : -INFINITY;
+__device__ __forceinline__ void row_emit(const ChunkArgs& a, const ChunkItem& it, int h, int row, int d, float m, float l, f32x4 o) {
+  if (it.splits > 1) {
+    float* dst = a.part + (((size_t)blockIdx.x * a.Hkv + h) * a.p.R + (row - it.rc * a.p.R)) * (D + 4);
+    *reinterpret_cast<f32x4*>(dst + d) = o;
+    if (d == 0) {
+      dst[D] = m;
+      dst[D + 1] = l;
+    }
     return;
   }
-  float* dst = a.part + (((size_t)blockIdx.x * a.Hkv + h) * a.p.R + (row - it.rc * a.p.R)) * (D + 4);
-  dst[d] = o;
-  if (d == 0) {
-    dst[D] = m;
-    dst[D + 1] = l;
+  const int G = a.p.G, i = row / G, hq = h * G + row - i * G;
+  const bool some = l > 0.f || l != l;
+  const float inv = some ? 1.f / l : 0.f;
+  T* O = static_cast<T*>(a.O) + ((size_t)(it.e.row0 + i) * a.Hq + hq) * D + d;
+  if constexpr (sizeof(T) == 2) {
+    bf16x4 v;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = (__bf16)(o[k] * inv);
+    *reinterpret_cast<bf16x4*>(O) = v;
+  } else {
+    *reinterpret_cast<f32x4*>(O) = o * inv;
   }
+  if (a.lse && d == 0) a.lse[(size_t)hq * a.r.total + it.e.row0 + i] = some ? m * 0.6931471805599453f + logf(l) : -INFINITY;
 }
 
 // The waves' states of 16 rows (sm_o [wave][16][D + 4], sm_ml [wave][16][2]) to row_emit; row0: the first of them, rows of the request.
-template <typename T, int D>
+template <typename T, int D, int NW>
 __device__ __forceinline__ void merge_waves(const ChunkArgs& a, const ChunkItem& it, int h, int row0, const float* sm_o, const float (*sm_ml)[16][2]) {
   const int rows = min(16, min((it.rc + 1) * a.p.R, it.e.n * a.p.G) - row0);
-  for (int idx = threadIdx.x; idx < rows * D; idx += kRowThreads) {
-    const int r = idx / D, d = idx % D;
+  for (int idx = threadIdx.x; idx < rows * (D / 4); idx += 64 * NW) {
+    const int r = idx / (D / 4), d = idx % (D / 4) * 4;
     float mm = sm_ml[0][r][0];
 #pragma unroll
-    for (int w = 1; w < kRowWaves; ++w) mm = fmaxf(mm, sm_ml[w][r][0]);
-    float ll = 0.f, oo = 0.f;
+    for (int w = 1; w < NW; ++w) mm = fmaxf(mm, sm_ml[w][r][0]);
+    float ll = 0.f;
+    f32x4 oo = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int w = 0; w < kRowWaves; ++w) {
+    for (int w = 0; w < NW; ++w) {
       const float f = __builtin_amdgcn_exp2f(sm_ml[w][r][0] - mm);
       ll += sm_ml[w][r][1] * f;
-      oo += sm_o[(w * 16 + r) * (D + 4) + d] * f;
+      oo += *reinterpret_cast<const f32x4*>(sm_o + (w * 16 + r) * (D + 4) + d) * f;
     }
     row_emit<T, D>(a, it, h, row0 + r, d, mm, ll, oo);
   }
@@ -141,7 +148,12 @@ void launch_chunk_merge(const ChunkArgs& a, int items, int rows, hipStream_t s) 
   if (a.p.max_splits > 1) hipLaunchKernelGGL((chunk_merge_kernel<T, D>), dim3(items, a.Hkv, rows < 16 ? rows : 16), dim3(kMergeThreads), 0, s, a);
 }
 
-hipError_t launch_chunk_bf16(const ChunkArgs& a, int D, int rows16, int items, int rows, hipStream_t s);
-hipError_t launch_chunk_f32(const ChunkArgs& a, int D, int rows16, int items, int rows, hipStream_t s);
+// How a call with few rows is launched: waves per workgroup, tiles of 16 rows, rows that a chunk can have, items.
+struct RowPlan {
+  ChunkPlan p;
+  int waves, rows16, rows, items;
+};
+hipError_t launch_chunk_bf16(const ChunkArgs& a, int D, const RowPlan& r, hipStream_t s);
+hipError_t launch_chunk_f32(const ChunkArgs& a, int D, const RowPlan& r, hipStream_t s);
 
 }  // namespace seka

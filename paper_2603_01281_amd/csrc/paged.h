@@ -143,11 +143,9 @@ __device__ __forceinline__ float groups_sum(float v) {
   return over_groups(v, [](float x, float y) __attribute__((always_inline)) { return x + y; });
 }
 
-constexpr int kRowWaves = 4;             // waves of a workgroup that take a range's blocks of keys in turn
-
-// Pages of a wave's next blocks of keys, one per lane: block n of the window is tokens k + 32 kRowWaves n .. + 31 (KEYS = 32).  A page
+// Pages of a wave's next blocks of keys, one per lane; NW waves take blocks of KEYS keys in turn.  A page
 // that is shorter than a block takes several lanes.
-template <int KEYS>
+template <int KEYS, int NW>
 struct PageWindow {
   int entry;             // this lane's page
   int per_block;         // lanes per block
@@ -158,7 +156,7 @@ struct PageWindow {
     const int shift = min(c.shift, __builtin_ctz(KEYS));
     per_block = KEYS >> shift;
     left = 64 / per_block;
-    const int j = key + (lane / per_block) * KEYS * kRowWaves + ((lane % per_block) << shift);
+    const int j = key + (lane / per_block) * KEYS * NW + ((lane % per_block) << shift);
     entry = page_of(c, b, min(j, k1 - 1));
   }
 };

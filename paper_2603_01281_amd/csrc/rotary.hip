@@ -7,6 +7,8 @@
 // HBM-bound: every row is read and written once.  A workgroup takes one token (grid.y: a share of its heads); one sine and cosine
 // per pair, which all heads of the token share, go through LDS while the first rows are on their way.  A thread owns whole pairs
 // (16 bytes on each side), so input and output may be the same memory.
+#include <algorithm>
+
 #include "paged.h"
 
 namespace seka {
@@ -26,37 +28,93 @@ template <> struct RotElem<float> {
   __device__ static float put(float x) { return x; }
 };
 
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+
+// Work of a token in units: V pairs of a row of Q or K, or V elements that are copied (behind the rotated part; V in the paged form).
+template <typename T, bool PAGED>
+struct RotUnit {
+  static constexpr int V = RotElem<T>::V;
+  enum Kind { PAIRS, PAIRS_BY_ELEMENT, COPY, COPY_BY_ELEMENT };
+  Kind kind;
+  bool is_q, is_v;
+  int h, i0, i1, n;      // head; first elements; pairs or elements
+
+  __device__ __forceinline__ RotUnit(const RotaryArgs& a, int u) {
+    const int dim = 2 * a.half, nrot = (a.half + V - 1) / V, per_row = nrot + (a.D - dim + V - 1) / V;
+    const int q_rows = a.Q ? a.Hq : 0, k_rows = a.K ? a.Hkv : 0, turned = (q_rows + k_rows) * per_row;
+    is_v = PAGED && u >= turned;
+    if (is_v) {
+      const int pieces = a.D / V, x = u - turned;
+      is_q = false;
+      h = x / pieces;
+      i0 = i1 = x % pieces * V;
+      n = V;
+      kind = COPY;
+      return;
+    }
+    const int row = u / per_row, part = u - row * per_row;
+    is_q = row < q_rows;
+    h = is_q ? row : row - q_rows;
+    if (part >= nrot) {
+      i0 = i1 = dim + (part - nrot) * V;
+      n = min(V, a.D - i0);
+      kind = dim % V == 0 ? COPY : COPY_BY_ELEMENT;
+    } else {
+      const int p0 = part * V;
+      n = min(V, a.half - p0);
+      i0 = a.interleaved ? 2 * p0 : p0;
+      i1 = a.interleaved ? 2 * p0 + V : a.half + p0;
+      kind = n == V && (a.interleaved || a.half % V == 0) ? PAIRS : PAIRS_BY_ELEMENT;
+    }
+  }
+  __device__ __forceinline__ static int count(const RotaryArgs& a) {
+    const int dim = 2 * a.half, per_row = (a.half + V - 1) / V + (a.D - dim + V - 1) / V;
+    return ((a.Q ? a.Hq : 0) + (a.K ? a.Hkv : 0)) * per_row + (PAGED ? a.Hkv * (a.D / V) : 0);
+  }
+  __device__ __forceinline__ const T* source(const RotaryArgs& a, int t) const {
+    const void* x = is_v ? a.V : is_q ? a.Q : a.K;
+    return static_cast<const T*>(x) + ((size_t)t * (is_q ? a.Hq : a.Hkv) + h) * a.D;
+  }
+};
+
 template <typename T, bool PAGED>
 __global__ __launch_bounds__(kRotThreads) void rotary_kernel(RotaryArgs a) {
   using E = RotElem<T>;
+  using Unit = RotUnit<T, PAGED>;
   constexpr int V = E::V;
-  typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
   __shared__ float cs[64], sn[64];
   const int t = blockIdx.x, tid = threadIdx.x;
+  const int units = Unit::count(a), stride = gridDim.y * kRotThreads;
+
+  // the first unit's loads are on their way while the token's place and its angles are found
+  int u = blockIdx.y * kRotThreads + tid;
+  Unit x(a, min(u, units - 1));
+  u32x4 v0 = {0, 0, 0, 0}, v1 = {0, 0, 0, 0};
+  auto load = [&]() __attribute__((always_inline)) {
+    const T* src = x.source(a, t);
+    if (x.kind == Unit::PAIRS || x.kind == Unit::COPY) v0 = *reinterpret_cast<const u32x4*>(src + x.i0);
+    if (x.kind == Unit::PAIRS) v1 = *reinterpret_cast<const u32x4*>(src + x.i1);
+  };
+  if (u < units) load();
 
   // ---- where the token lies ----
-  bool owned = true, cached = false;
-  int slot = 0, page = 0;
-  int pos = 0;
+  bool cached = false;
+  int slot = 0, page = 0, pos = 0;
   if (PAGED) {
     // the request is the number of requests that end at or before row t
     int b = 0;
     for (int b0 = 0; b0 < a.r.B; b0 += kRotThreads)
       b += __syncthreads_count(b0 + tid < a.r.B && a.r.cu[min(b0 + tid, a.r.B - 1) + 1] <= t);
-    owned = b < a.r.B;
-    if (owned) {
-      const ChunkExtent e = chunk_extent(a.r, a.c, b);
-      const int i = t - e.row0;
-      owned = i >= 0 && i < e.n;
-      const int j = e.len - e.n + i;
-      cached = owned && j >= 0;
-      if (cached) {
-        page = page_of(a.c, b, j);
-        slot = j & ((1 << a.c.shift) - 1);
-      }
-      pos = j;
+    if (b >= a.r.B) return;                  // the same in every thread
+    const ChunkExtent e = chunk_extent(a.r, a.c, b);
+    const int i = t - e.row0, j = e.len - e.n + i;
+    if (i < 0 || i >= e.n) return;
+    cached = j >= 0;
+    if (cached) {
+      page = page_of(a.c, b, j);
+      slot = j & ((1 << a.c.shift) - 1);
     }
-    if (!owned) return;                      // the same in every thread
+    pos = j;
   } else {
     pos = t % a.S;
   }
@@ -72,89 +130,72 @@ __global__ __launch_bounds__(kRotThreads) void rotary_kernel(RotaryArgs a) {
   }
   __syncthreads();
 
-  // ---- units: V pairs each, then pieces of V elements that are copied ----
-  const int dim = 2 * a.half;
-  const int nrot = (a.half + V - 1) / V;
-  const bool vec_pairs = a.interleaved ? dim % (2 * V) == 0 : a.half % V == 0;
-  const int ncopy = (a.D - dim + V - 1) / V;
-  const bool vec_copy = dim % V == 0;
-  const int per_row = nrot + ncopy;
-  const int q_rows = a.Q ? a.Hq : 0, k_rows = a.K ? a.Hkv : 0, v_rows = PAGED ? a.Hkv : 0;
-  const int units = (q_rows + k_rows) * per_row;
   const size_t cache_row = ((((size_t)page << a.c.shift) + slot) * a.Hkv) * a.D;
-  for (int u = blockIdx.y * kRotThreads + tid; u < units; u += gridDim.y * kRotThreads) {
-    const int row = u / per_row, part = u % per_row;
-    const bool is_q = row < q_rows;
-    const int h = is_q ? row : row - q_rows;
-    if (PAGED && !is_q && !cached) continue;
-    const T* src = is_q ? static_cast<const T*>(a.Q) + ((size_t)t * a.Hq + h) * a.D : static_cast<const T*>(a.K) + ((size_t)t * a.Hkv + h) * a.D;
-    T* dst = is_q ? static_cast<T*>(a.Q_out) + ((size_t)t * a.Hq + h) * a.D
-             : PAGED ? static_cast<T*>(a.c.K) + cache_row + (size_t)h * a.D
-                     : static_cast<T*>(a.K_out) + ((size_t)t * a.Hkv + h) * a.D;
-    if (part >= nrot) {                      // behind the rotated part
-      if (src == dst) continue;
-      const int e0 = dim + (part - nrot) * V;
-      if (vec_copy) {
-        *reinterpret_cast<u32x4*>(dst + e0) = *reinterpret_cast<const u32x4*>(src + e0);
-      } else {
-        for (int e = e0; e < min(e0 + V, a.D); ++e) dst[e] = src[e];
-      }
-      continue;
-    }
-    const int p0 = part * V;
-    if (vec_pairs) {
-      const int i0 = a.interleaved ? 2 * p0 : p0, i1 = a.interleaved ? 2 * p0 + V : a.half + p0;
-      u32x4 v0 = *reinterpret_cast<const u32x4*>(src + i0), v1 = *reinterpret_cast<const u32x4*>(src + i1);
-      T x[V], y[V];
-      __builtin_memcpy(x, &v0, 16);
-      __builtin_memcpy(y, &v1, 16);
+  while (u < units) {
+    const T* src = x.source(a, t);
+    T* dst = x.is_q ? static_cast<T*>(a.Q_out) + ((size_t)t * a.Hq + x.h) * a.D
+             : PAGED ? static_cast<T*>(x.is_v ? a.c.V : a.c.K) + cache_row + (size_t)x.h * a.D
+                     : static_cast<T*>(a.K_out) + ((size_t)t * a.Hkv + x.h) * a.D;
+    const int p0 = a.interleaved ? x.i0 / 2 : x.i0;
+    if (PAGED && !x.is_q && !cached) {
+      // a token that has no place in the cache
+    } else if (x.kind == Unit::PAIRS) {
+      T p[V], q[V];
+      __builtin_memcpy(p, &v0, 16);
+      __builtin_memcpy(q, &v1, 16);
       if (a.interleaved) {
 #pragma unroll
         for (int k = 0; k < V; k += 2) {
-          const int p = p0 + k / 2, q = p + V / 2;
-          const float x0 = E::get(x[k]), x1 = E::get(x[k + 1]), y0 = E::get(y[k]), y1 = E::get(y[k + 1]);
-          x[k] = E::put(x0 * cs[p] - x1 * sn[p]);
-          x[k + 1] = E::put(x1 * cs[p] + x0 * sn[p]);
-          y[k] = E::put(y0 * cs[q] - y1 * sn[q]);
-          y[k + 1] = E::put(y1 * cs[q] + y0 * sn[q]);
+          const int i = p0 + k / 2, j = i + V / 2;
+          const float x0 = E::get(p[k]), x1 = E::get(p[k + 1]), y0 = E::get(q[k]), y1 = E::get(q[k + 1]);
+          p[k] = E::put(x0 * cs[i] - x1 * sn[i]);
+          p[k + 1] = E::put(x1 * cs[i] + x0 * sn[i]);
+          q[k] = E::put(y0 * cs[j] - y1 * sn[j]);
+          q[k + 1] = E::put(y1 * cs[j] + y0 * sn[j]);
         }
       } else {
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-          const float x0 = E::get(x[k]), y0 = E::get(y[k]);
-          x[k] = E::put(x0 * cs[p0 + k] - y0 * sn[p0 + k]);
-          y[k] = E::put(y0 * cs[p0 + k] + x0 * sn[p0 + k]);
+          const float x0 = E::get(p[k]), y0 = E::get(q[k]);
+          p[k] = E::put(x0 * cs[p0 + k] - y0 * sn[p0 + k]);
+          q[k] = E::put(y0 * cs[p0 + k] + x0 * sn[p0 + k]);
         }
       }
-      __builtin_memcpy(&v0, x, 16);
-      __builtin_memcpy(&v1, y, 16);
-      *reinterpret_cast<u32x4*>(dst + i0) = v0;
-      *reinterpret_cast<u32x4*>(dst + i1) = v1;
+      __builtin_memcpy(&v0, p, 16);
+      __builtin_memcpy(&v1, q, 16);
+      *reinterpret_cast<u32x4*>(dst + x.i0) = v0;
+      *reinterpret_cast<u32x4*>(dst + x.i1) = v1;
+    } else if (x.kind == Unit::COPY) {
+      if (src != dst) *reinterpret_cast<u32x4*>(dst + x.i0) = v0;
+    } else if (x.kind == Unit::COPY_BY_ELEMENT) {
+      if (src != dst)
+        for (int e = 0; e < x.n; ++e) dst[x.i0 + e] = src[x.i0 + e];
     } else {
-      for (int p = p0; p < min(p0 + V, a.half); ++p) {
-        const int i0 = a.interleaved ? 2 * p : p, i1 = a.interleaved ? 2 * p + 1 : a.half + p;
-        const float x0 = E::get(src[i0]), y0 = E::get(src[i1]);
-        dst[i0] = E::put(x0 * cs[p] - y0 * sn[p]);
-        dst[i1] = E::put(y0 * cs[p] + x0 * sn[p]);
+      for (int k = 0; k < x.n; ++k) {
+        const int e0 = a.interleaved ? x.i0 + 2 * k : x.i0 + k, e1 = a.interleaved ? e0 + 1 : x.i1 + k;
+        const float x0 = E::get(src[e0]), y0 = E::get(src[e1]);
+        dst[e0] = E::put(x0 * cs[p0 + k] - y0 * sn[p0 + k]);
+        dst[e1] = E::put(y0 * cs[p0 + k] + x0 * sn[p0 + k]);
       }
     }
-  }
-  if (PAGED && cached) {
-    const int pieces = a.D / V;
-    for (int u = blockIdx.y * kRotThreads + tid; u < v_rows * pieces; u += gridDim.y * kRotThreads) {
-      const size_t e0 = (size_t)u * V;
-      *reinterpret_cast<u32x4*>(static_cast<T*>(a.c.V) + cache_row + e0) =
-          *reinterpret_cast<const u32x4*>(static_cast<const T*>(a.V) + (size_t)t * a.Hkv * a.D + e0);
+    u += stride;
+    if (u < units) {
+      x = Unit(a, u);
+      load();
     }
-    if (a.c.W && blockIdx.y == 0 && tid < a.Hkv)
-      a.c.W[((size_t)page * a.Hkv + tid) * (1 << a.c.shift) + slot] = a.mask && a.mask[t] ? INFINITY : 0.f;
   }
+  if (PAGED && cached && a.c.W && blockIdx.y == 0 && tid < a.Hkv)
+    a.c.W[((size_t)page * a.Hkv + tid) * (1 << a.c.shift) + slot] = a.mask && a.mask[t] ? INFINITY : 0.f;
 }
 
 }  // namespace
 
 hipError_t launch_rotary(const RotaryArgs& a, int dtype, hipStream_t s) {
-  const dim3 grid(a.total, 1), block(kRotThreads);
+  // a workgroup per token, and where those are few so many that every thread has one unit: the rest is waiting for memory
+  const int row_units = (a.D + 15) / 16 * (dtype == SEKA_BF16 ? 1 : 2) + 1;
+  const int units = ((a.Q ? a.Hq : 0) + 2 * (a.K ? a.Hkv : 0)) * row_units;
+  const int most = std::max(1, (units + kRotThreads - 1) / kRotThreads);
+  const dim3 grid(a.total, std::min(most, std::max(1, 1024 / a.total))), block(kRotThreads);
   if (a.r.B > 0) {
     if (dtype == SEKA_BF16) hipLaunchKernelGGL((rotary_kernel<uint16_t, true>), grid, block, 0, s, a);
     else hipLaunchKernelGGL((rotary_kernel<float, true>), grid, block, 0, s, a);

@@ -101,13 +101,13 @@ __device__ __forceinline__ void wt_arrived(F (&kf)[KT][NF]) {
 // ---- few rows ------------------------------------------------------------------------------------------------------------
 
 template <typename T, int D, int RT>
-__global__ __launch_bounds__(kRowWaves * 64, 2) void weights_stream_kernel(WeightsArgs a) {
+__global__ __launch_bounds__(kWtThreads, 2) void weights_stream_kernel(WeightsArgs a) {
   typedef typename WtMath<T>::frag frag;
   constexpr int RB = D * sizeof(T), NF = RB / 64;                       // bytes of a row, fragments of it: 64 bytes over four lanes each
   constexpr int BK = sizeof(T) == 2 ? 32 : 16, KT = BK / 16;
   constexpr int CPR = RB / 16, RPI = 64 / CPR, NV = BK / RPI;           // 16-byte pieces per row, rows per load, loads per block
   constexpr int LD = RB + 16;                                           // LDS row stride (bytes): 16 rows at one piece, spread over all banks
-  __shared__ __attribute__((aligned(16))) unsigned char smem[kRowWaves * BK * LD];
+  __shared__ __attribute__((aligned(16))) unsigned char smem[kWtWaves * BK * LD];
 
   ChunkItem it;
   if (!plan_item(a.r, a.c, a.p, blockIdx.x, it)) return;
@@ -152,7 +152,7 @@ __global__ __launch_bounds__(kRowWaves * 64, 2) void weights_stream_kernel(Weigh
   u32x4 kr[NV];
   float w_in = 0.f;
   size_t home = 0, home_next = 0;          // of key kb + lane, lane < BK
-  PageWindow<BK> win;
+  PageWindow<BK, kWtWaves> win;
   int block = 0;
   auto fetch = [&](int kb) __attribute__((always_inline)) {
     if (block == win.left) {
@@ -187,13 +187,13 @@ __global__ __launch_bounds__(kRowWaves * 64, 2) void weights_stream_kernel(Weigh
     win.load(a.c, it.b, kb, k1);
     fetch(kb);
   }
-  for (; kb < k1; kb += kRowWaves * BK) {
+  for (; kb < k1; kb += kWtWaves * BK) {
 #pragma unroll
     for (int x = 0; x < NV; ++x) *reinterpret_cast<u32x4*>(tile + (RPI * x + lane / CPR) * LD + 16 * (lane % CPR)) = kr[x];
     asm volatile("" ::: "memory");         // (a wave's LDS operations execute in program order)
     const float w = w_in;
     home = home_next;
-    if (kb + kRowWaves * BK < k1) fetch(kb + kRowWaves * BK);
+    if (kb + kWtWaves * BK < k1) fetch(kb + kWtWaves * BK);
     float sum[KT];
     frag k[KT][NF];
 #pragma unroll
@@ -424,9 +424,9 @@ hipError_t launch(WeightsArgs a, hipStream_t s) {
     a.p.max_splits = std::max(1, (a.c.cap + 255) / 256);
     const int items = (int)std::min((long long)a.r.B + (1 << a.p.slots_log2), (long long)a.r.B * a.p.max_splits);
     const dim3 grid(items, a.Hkv);
-    if (rows <= 16) hipLaunchKernelGGL((weights_stream_kernel<T, D, 1>), grid, dim3(64 * kRowWaves), 0, s, a);
-    else if (rows <= 32) hipLaunchKernelGGL((weights_stream_kernel<T, D, 2>), grid, dim3(64 * kRowWaves), 0, s, a);
-    else hipLaunchKernelGGL((weights_stream_kernel<T, D, kFew / 16>), grid, dim3(64 * kRowWaves), 0, s, a);
+    if (rows <= 16) hipLaunchKernelGGL((weights_stream_kernel<T, D, 1>), grid, threads, 0, s, a);
+    else if (rows <= 32) hipLaunchKernelGGL((weights_stream_kernel<T, D, 2>), grid, threads, 0, s, a);
+    else hipLaunchKernelGGL((weights_stream_kernel<T, D, kFew / 16>), grid, threads, 0, s, a);
     return hipGetLastError();
   }
   constexpr int KEYS = 16 * wt_tiles<T, D>();

@@ -20,14 +20,16 @@ def run(seka, x, lse=True, max_q=None, max_len=None, scale=0.0, workspace=None, 
 
 
 def check(seka, x, what, **kw):
-    O, L = run(seka, x, **kw)
     print(what, flush=True)
     used = int(x.cu[-1])
-    scale = kw.get("scale") or None
-    ref = orc.chunk_attention(x.Q, x.K, x.V, x.table, x.lens, x.cu, scale=scale)
+    ref = orc.chunk_attention(x.Q, x.K, x.V, x.table, x.lens, x.cu, scale=kw.get("scale") or None)
     ref = (ref[0][:used], ref[1][:, :used], ref[2][:used], ref[3][:, :used])
-    P.check_attention(P.f64(O)[:used], P.f64(L)[:, :used] if L is not None else None, ref, x.dtype, what, lse=L is not None)
-    assert (O[used:] == 7.0).all() and (L is None or (L[:, used:] == 7.0).all()), f"{what}: rows behind the last request were written"
+    # chunks that are long enough for it: also with the kernel of long caches, which a bound on the cached tokens asks for
+    far = x.dtype == "bf16" and max(x.new) * x.Hq // x.Hkv > 64 and "max_len" not in kw
+    for more in ({}, dict(max_len=min(100000, (1 << 31) // (x.Hq * x.D) - 1))) if far else ({},):
+        O, L = run(seka, x, **kw, **more)
+        P.check_attention(P.f64(O)[:used], P.f64(L)[:, :used] if L is not None else None, ref, x.dtype, f"{what} {more}", lse=L is not None)
+        assert (O[used:] == 7.0).all() and (L is None or (L[:, used:] == 7.0).all()), f"{what}: rows behind the last request were written"
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
