@@ -427,7 +427,7 @@ class PagedCache:
         if any(t.device != K.device for t in (V, table, lens)) or (W is not None and W.device != K.device):
             raise ValueError("the tensors of a cache must be on one device")
         self.K, self.V, self.table, self.lens, self.W = K, V, table, lens, W
-        self.dtype, self.device, self.code = K.dtype, K.device, _dtype_code(K)
+        self.dtype, self.index, self.code = K.dtype, K.get_device(), _dtype_code(K)
         self.B, self.capacity = table.shape[0], table.shape[1] * self.page_size
         self.struct = seka_paged(_dev(K, "K"), _dev(V, "V"), _dev(W, "W"), _dev(table, "table"), _dev(lens, "lens"), pages, self.page_size,
                                  table.shape[1])
@@ -439,30 +439,47 @@ def paged_cache(K, V, table, lens, W=None):
     return PagedCache(K, V, table, lens, W)
 
 
-def _chunk(X, cache, cu_seqlens, heads, name):
-    """Checks of a packed tensor against its cache; returns its pointer."""
-    if X.dim() != 3 or X.shape[2] != cache.D or X.dtype != cache.dtype or (heads is not None and X.shape[1] != heads):
-        raise ValueError(f"{name} must be [total, {'heads' if heads is None else heads}, {cache.D}] of dtype {cache.dtype}")
-    if cu_seqlens.dtype != torch.int32 or cu_seqlens.numel() != cache.B + 1:
-        raise ValueError(f"cu_seqlens must be int32 [B + 1 = {cache.B + 1}]")
-    if X.device != cache.device:
-        raise ValueError(f"{name} must be on the cache's device")
-    return _dev(X, name)
+def _rows(X, total, heads, cache, name):
+    """Pointer of a packed tensor that belongs to a cache.  (Few attribute accesses: for a generation step they are the call's time.)"""
+    if X.shape != (total, heads, cache.D) or X.dtype is not cache.dtype or X.get_device() != cache.index or not X.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous [{total}, {heads}, {cache.D}] of dtype {cache.dtype} on device {cache.index}, "
+                         f"got {tuple(X.shape)} {X.dtype} on {X.device}")
+    return X.data_ptr()
+
+
+def _of(X, dtype, n, cache, name):
+    """Pointer of an index, mask or length tensor of n entries, or None."""
+    if X is None:
+        return None
+    if X.dtype is not dtype or X.numel() != n or X.get_device() != cache.index or not X.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of {n} entries on device {cache.index}")
+    return X.data_ptr()
+
+
+def _current(cache, stream):
+    """The stream of a call over a cache: the launch goes to the current device, which has to be the cache's."""
+    if torch._C._cuda_getDevice() != cache.index:
+        raise ValueError(f"the cache is on device {cache.index}, the current device is {torch._C._cuda_getDevice()}")
+    return torch._C._cuda_getCurrentRawStream(cache.index) if stream is None else stream
 
 
 def seka_rotary(Q, Q_out, rope, K=None, K_out=None, positions=None, stream=None):
     """Q/Q_out [B,S,Hq,D], K/K_out [B,S,Hkv,D] or None; outputs may be the inputs.  positions [B,S] int32 device tensor or None."""
     B, S, Hq, D = Q.shape
-    if Q_out.shape != Q.shape or Q_out.dtype != Q.dtype:
+    if Q_out.shape != Q.shape or Q_out.dtype is not Q.dtype:
         raise ValueError("Q_out must be like Q")
     Hkv = 1
     if K is not None:
-        if K.shape[:2] != Q.shape[:2] or K.shape[3] != D or K.dtype != Q.dtype or K_out is None or K_out.shape != K.shape or K_out.dtype != K.dtype:
-            raise ValueError("K and K_out must be [B, S, Hkv, D] of Q's dtype")
         Hkv = K.shape[2]
-    if positions is not None and (positions.dtype != torch.int32 or positions.numel() != B * S):
+        if K.shape != (B, S, Hkv, D) or K.dtype is not Q.dtype or K_out is None or K_out.shape != K.shape or K_out.dtype is not K.dtype:
+            raise ValueError("K and K_out must be [B, S, Hkv, D] of Q's dtype")
+    if positions is not None and (positions.dtype is not torch.int32 or positions.numel() != B * S):
         raise ValueError("positions must be int32, one per token")
-    sh = _shape(B, S, Hq, Hkv, D, _dtype_code(Q), 0.0)
+    at = torch._C._cuda_getDevice()
+    for x in (Q, Q_out, K, K_out, positions):
+        if x is not None and x.get_device() != at:
+            raise ValueError(f"the tensors must be on the current device, {at}")
+    sh = seka_shape(B, S, Hq, Hkv, D, _dtype_code(Q), 0.0)
     _check(lib.seka_rotary(_dev(Q, "Q"), _dev(Q_out, "Q_out"), _dev(K, "K"), _dev(K_out, "K_out"), ctypes.byref(sh), rope.ref,
                            _dev(positions, "positions"), _stream(stream)))
     return Q_out
@@ -471,22 +488,15 @@ def seka_rotary(Q, Q_out, rope, K=None, K_out=None, positions=None, stream=None)
 def seka_cache_append(K, V, cache, cu_seqlens, max_q, rope=None, positions=None, Q=None, Q_out=None, mask=None, max_len=None, stream=None):
     """K/V [total,Hkv,D] into the pages, turned by rope if given; Q [total,Hq,D] -> Q_out turned beside them.  positions [total]
     int32 or None (index in the cache); mask [total] uint8 or None; max_len: the most cached tokens (the table's capacity if None)."""
-    total = K.shape[0]
-    k, v = _chunk(K, cache, cu_seqlens, cache.Hkv, "K"), _chunk(V, cache, cu_seqlens, cache.Hkv, "V")
-    Hq = cache.Hkv
-    q = qo = None
+    total, Hq, q, qo = K.shape[0], cache.Hkv, None, None
     if Q is not None:
         Hq = Q.shape[1]
-        q, qo = _chunk(Q, cache, cu_seqlens, Hq, "Q"), _chunk(Q_out, cache, cu_seqlens, Hq, "Q_out")
-    if V.shape[0] != total or (Q is not None and (Q.shape[0] != total or Q_out.shape[0] != total)):
-        raise ValueError("K, V, Q and Q_out must have one row per new token")
-    if positions is not None and (positions.dtype != torch.int32 or positions.numel() != total):
-        raise ValueError("positions must be int32, one per new token")
-    if mask is not None and (mask.dtype != torch.uint8 or mask.numel() != total):
-        raise ValueError("mask must be uint8, one per new token")
-    sh = _shape(cache.B, cache.capacity if max_len is None else max_len, Hq, cache.Hkv, cache.D, cache.code, 0.0)
-    _check(lib.seka_cache_append(k, v, q, qo, ctypes.byref(sh), cache.ref, rope.ref if rope is not None else None, _dev(positions, "positions"),
-                                 _dev(mask, "mask"), _dev(cu_seqlens, "cu_seqlens"), total, max_q, _stream(stream)))
+        q, qo = _rows(Q, total, Hq, cache, "Q"), _rows(Q_out, total, Hq, cache, "Q_out")
+    sh = seka_shape(cache.B, cache.capacity if max_len is None else max_len, Hq, cache.Hkv, cache.D, cache.code, 0.0)
+    _check(lib.seka_cache_append(_rows(K, total, cache.Hkv, cache, "K"), _rows(V, total, cache.Hkv, cache, "V"), q, qo, ctypes.byref(sh), cache.ref,
+                                 None if rope is None else rope.ref, _of(positions, torch.int32, total, cache, "positions"),
+                                 _of(mask, torch.uint8, total, cache, "mask"), _of(cu_seqlens, torch.int32, cache.B + 1, cache, "cu_seqlens"), total,
+                                 max_q, _current(cache, stream)))
 
 
 def seka_chunk_workspace_bytes(B, S, Hq, Hkv, D, dtype, total_tokens, max_q):
@@ -498,15 +508,14 @@ def seka_attention_chunk(Q, O, cache, cu_seqlens, max_q, max_len=None, lse=None,
     """Q/O [total,Hq,D]; cu_seqlens [B+1] int32 device tensor; max_q: the longest chunk; max_len: the most cached tokens (the
     table's capacity if None); lse [Hq,total] fp32 or None."""
     total, Hq, _ = Q.shape
-    q, o = _chunk(Q, cache, cu_seqlens, Hq, "Q"), _chunk(O, cache, cu_seqlens, Hq, "O")
-    if O.shape[0] != total or (lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (Hq, total))):
-        raise ValueError(f"O must be like Q, lse fp32 [Hq={Hq}, total={total}]")
-    sh = _shape(cache.B, cache.capacity if max_len is None else max_len, Hq, cache.Hkv, cache.D, cache.code, scale)
+    sh = seka_shape(cache.B, cache.capacity if max_len is None else max_len, Hq, cache.Hkv, cache.D, cache.code, scale)
+    if lse is not None and lse.shape != (Hq, total):
+        raise ValueError(f"lse must be [Hq={Hq}, total={total}]")
     if workspace is None:
-        need = lib.seka_chunk_workspace_bytes(ctypes.byref(sh), total, max_q)
-        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=Q.device)
-    _check(lib.seka_attention_chunk(q, o, _dev(lse, "lse"), ctypes.byref(sh), cache.ref, _dev(cu_seqlens, "cu_seqlens"), total, max_q,
-                                    _dev(workspace, "workspace"), workspace.numel() * workspace.element_size(), _stream(stream)))
+        workspace = torch.empty(max(lib.seka_chunk_workspace_bytes(ctypes.byref(sh), total, max_q), 16), dtype=torch.uint8, device=Q.device)
+    _check(lib.seka_attention_chunk(_rows(Q, total, Hq, cache, "Q"), _rows(O, total, Hq, cache, "O"), _of(lse, torch.float32, Hq * total, cache, "lse"),
+                                    ctypes.byref(sh), cache.ref, _of(cu_seqlens, torch.int32, cache.B + 1, cache, "cu_seqlens"), total, max_q,
+                                    _dev(workspace, "workspace"), workspace.numel() * workspace.element_size(), _current(cache, stream)))
     return O
 
 
@@ -514,29 +523,29 @@ def seka_attention_weights(Q, lse, cache, cu_seqlens, max_q, max_len=None, windo
     """Writes cache.W: decay * W_in (zeros if None) plus the attention that every cached token gets from the last `window` new
     tokens (all if None) of every chunk.  Q [total,Hq,D], lse [Hq,total] of seka_attention_chunk."""
     total, Hq, _ = Q.shape
-    q = _chunk(Q, cache, cu_seqlens, Hq, "Q")
-    if lse.dtype != torch.float32 or tuple(lse.shape) != (Hq, total):
-        raise ValueError(f"lse must be fp32 [Hq={Hq}, total={total}]")
-    if W_in is not None and (cache.W is None or W_in.dtype != torch.float32 or W_in.shape != cache.W.shape):
+    if lse.shape != (Hq, total):
+        raise ValueError(f"lse must be [Hq={Hq}, total={total}]")
+    if W_in is not None and (cache.W is None or W_in.shape != cache.W.shape):
         raise ValueError("W_in must be like the cache's W")
-    sh = _shape(cache.B, cache.capacity if max_len is None else max_len, Hq, cache.Hkv, cache.D, cache.code, scale)
-    _check(lib.seka_attention_weights(q, _dev(lse, "lse"), ctypes.byref(sh), cache.ref, _dev(W_in, "W_in"), _dev(cu_seqlens, "cu_seqlens"),
-                                      total, max_q, max_q if window is None else window, float(decay), _stream(stream)))
+    sh = seka_shape(cache.B, cache.capacity if max_len is None else max_len, Hq, cache.Hkv, cache.D, cache.code, scale)
+    _check(lib.seka_attention_weights(_rows(Q, total, Hq, cache, "Q"), _of(lse, torch.float32, Hq * total, cache, "lse"), ctypes.byref(sh), cache.ref,
+                                      None if W_in is None else _of(W_in, torch.float32, cache.W.numel(), cache, "W_in"),
+                                      _of(cu_seqlens, torch.int32, cache.B + 1, cache, "cu_seqlens"), total, max_q, max_q if window is None else window,
+                                      decay, _current(cache, stream)))
     return cache.W
 
 
 def seka_cache_evict(src, dst, kept, recent, lens_out=None, max_len=None, stream=None):
     """Cuts src's caches to kept.shape[2] tokens per head, into dst's pages (src itself: in place).  kept [B,Hkv,budget] int32;
     lens_out [B] int32 (dst.lens if None; not src.lens).  Returns lens_out."""
-    if (dst.B, dst.Hkv, dst.D, dst.dtype) != (src.B, src.Hkv, src.D, src.dtype):
-        raise ValueError("src and dst must have the same requests, heads and dtype")
-    if kept.dtype != torch.int32 or kept.dim() != 3 or tuple(kept.shape[:2]) != (src.B, src.Hkv):
-        raise ValueError(f"kept must be int32 [B={src.B}, Hkv={src.Hkv}, budget]")
+    if (dst.B, dst.Hkv, dst.D, dst.dtype, dst.index) != (src.B, src.Hkv, src.D, src.dtype, src.index):
+        raise ValueError("src and dst must have the same requests, heads, dtype and device")
+    budget = kept.shape[2]
+    if kept.shape != (src.B, src.Hkv, budget):
+        raise ValueError(f"kept must be [B={src.B}, Hkv={src.Hkv}, budget]")
     if lens_out is None:
         lens_out = dst.lens
-    if lens_out.dtype != torch.int32 or lens_out.numel() != src.B:
-        raise ValueError(f"lens_out must be int32 [B={src.B}]")
-    sh = _shape(src.B, src.capacity if max_len is None else max_len, src.Hkv, src.Hkv, src.D, src.code, 0.0)
-    _check(lib.seka_cache_evict(ctypes.byref(sh), src.ref, dst.ref, kept.shape[2], recent, _dev(kept, "kept"), _dev(lens_out, "lens_out"),
-                                _stream(stream)))
+    sh = seka_shape(src.B, src.capacity if max_len is None else max_len, src.Hkv, src.Hkv, src.D, src.code, 0.0)
+    _check(lib.seka_cache_evict(ctypes.byref(sh), src.ref, dst.ref, budget, recent, _of(kept, torch.int32, src.B * src.Hkv * budget, src, "kept"),
+                                _of(lens_out, torch.int32, src.B, src, "lens_out"), _current(src, stream)))
     return lens_out

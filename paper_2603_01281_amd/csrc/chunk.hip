@@ -240,8 +240,8 @@ RowPlan row_plan(int B, int S, int Hq, int Hkv, int D, int dtype, int total, int
   while ((1 << r.p.slots_log2) * Hkv < (few ? 256 : 512)) ++r.p.slots_log2;
   r.p.least = bf16 ? 8 : 4;                // 256 tokens, 128: a block of every wave of eight
   r.p.max_splits = std::max(1, std::min(kMaxRanges, (blocks + r.p.least - 1) / r.p.least));
-  // and no second kernel where a wave has no more than four blocks
-  if (few && S <= (bf16 ? 1024 : 512)) r.p.max_splits = 1;
+  // and no second kernel where a wave has four blocks of bf16 keys, or eight of fp32 ones, at most
+  if (few && S <= 1024) r.p.max_splits = 1;
   r.p.streams = (long long)(300e6 / (2.0 * 32 * Hkv * D * (bf16 ? 2 : 4)));
   // sum over chunks of ceil(blocks / L) <= T / L + chunks with T / L <= slots, and no more than every chunk in all its ranges
   r.items = (int)std::min(chunks + (1 << r.p.slots_log2), chunks * r.p.max_splits);

@@ -145,7 +145,9 @@ __global__ __launch_bounds__(kMergeThreads) void chunk_merge_kernel(ChunkArgs a)
 // rows: of a chunk that exist, at most
 template <typename T, int D>
 void launch_chunk_merge(const ChunkArgs& a, int items, int rows, hipStream_t s) {
-  if (a.p.max_splits > 1) hipLaunchKernelGGL((chunk_merge_kernel<T, D>), dim3(items, a.Hkv, rows < 16 ? rows : 16), dim3(kMergeThreads), 0, s, a);
+  if (a.p.max_splits <= 1) return;
+  const int z = (long long)items * a.Hkv * rows <= 16384 || rows < 16 ? rows : 16;       // workgroups beyond that have several rows each
+  hipLaunchKernelGGL((chunk_merge_kernel<T, D>), dim3(items, a.Hkv, z), dim3(kMergeThreads), 0, s, a);
 }
 
 // How a call with few rows is launched: waves per workgroup, tiles of 16 rows, rows that a chunk can have, items.

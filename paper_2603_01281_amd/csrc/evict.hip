@@ -14,6 +14,7 @@
 namespace seka {
 namespace {
 
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64;
 constexpr int kSelCopies = 16;                  // of every counter: lanes that count the same byte meet in one of them
 constexpr int kSelKeys = 30 * 1024;             // tokens whose keys LDS holds
@@ -27,7 +28,7 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
 }
 
 __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(EvictArgs a) {
-  extern __shared__ uint32_t keys[];            // [min(candidates, kSelKeys)]
+  extern __shared__ __attribute__((aligned(16))) uint32_t keys[];            // [min(candidates, kSelKeys), whole quads]
   __shared__ __attribute__((aligned(16))) uint32_t hist[2][256 * kSelCopies];
   __shared__ __attribute__((aligned(16))) uint32_t total[2][256];
   __shared__ int sm_gt[kSelWaves], sm_eq[kSelWaves];
@@ -42,21 +43,30 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(EvictArgs a) 
   const int want = a.budget - a.recent;         // of them; < m
   for (int k = tid; k < a.recent; k += kSelThreads) kept[want + k] = m + k;
   if (want == 0) return;
-  const int shift = a.src.shift;
+  // tokens four at a time: a page has eight or more
+  const int shift = a.src.shift, quads = (m + 3) / 4;
   const bool held = m <= kSelKeys;
-  auto weight_at = [&](int j) __attribute__((always_inline)) -> float {
-    return a.src.W[(((size_t)page_of(a.src, b, j) * a.Hkv + h) << shift) + (j & ((1 << shift) - 1))];
+  auto weights_of = [&](int q) __attribute__((always_inline)) -> f32x4 {
+    const int j = 4 * q;
+    return *reinterpret_cast<const f32x4*>(a.src.W + (((size_t)page_of(a.src, b, j) * a.Hkv + h) << shift) + (j & ((1 << shift) - 1)));
   };
-  auto key_at = [&](int j) __attribute__((always_inline)) -> uint32_t { return held ? keys[j] : weight_key(weight_at(j)); };
-  if (held) {
-    constexpr int U = 8;                        // tokens of a thread whose loads are in flight together
-    for (int j0 = tid; j0 < m; j0 += U * kSelThreads) {
-      float w[U];
+  auto keys_of = [&](f32x4 w) __attribute__((always_inline)) -> u32x4 {
+    u32x4 k;
 #pragma unroll
-      for (int u = 0; u < U; ++u) w[u] = weight_at(min(j0 + u * kSelThreads, m - 1));
+    for (int x = 0; x < 4; ++x) k[x] = weight_key(w[x]);
+    return k;
+  };
+  u32x4* const keys4 = reinterpret_cast<u32x4*>(keys);
+  auto keys_at = [&](int q) __attribute__((always_inline)) -> u32x4 { return held ? keys4[q] : keys_of(weights_of(q)); };
+  if (held) {
+    constexpr int U = 4;                        // quads of a thread whose loads are in flight together
+    for (int q0 = tid; q0 < quads; q0 += U * kSelThreads) {
+      f32x4 w[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) w[u] = weights_of(min(q0 + u * kSelThreads, quads - 1));
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        if (j0 + u * kSelThreads < m) keys[j0 + u * kSelThreads] = weight_key(w[u]);
+        if (q0 + u * kSelThreads < quads) keys4[q0 + u * kSelThreads] = keys_of(w[u]);
     }
   }
   for (int k = tid; k < 256 * kSelCopies; k += kSelThreads) hist[0][k] = 0;
@@ -66,10 +76,12 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(EvictArgs a) 
   int need = want;                              // of the keys that begin with prefix
   for (int byte = 3; byte >= 0; --byte) {
     const int now = byte & 1 ? 0 : 1;           // counters of this byte; the others are cleared for the next one
-#pragma unroll 4
-    for (int j = tid; j < m; j += kSelThreads) {
-      const uint32_t u = key_at(j);
-      if (byte == 3 || (u >> (8 * byte + 8)) == prefix) atomicAdd(&hist[now][((u >> (8 * byte)) & 255) * kSelCopies + (lane & (kSelCopies - 1))], 1u);
+    for (int q = tid; q < quads; q += kSelThreads) {
+      const u32x4 u = keys_at(q);
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+        if (4 * q + x < m && (byte == 3 || (u[x] >> (8 * byte + 8)) == prefix))
+          atomicAdd(&hist[now][((u[x] >> (8 * byte)) & 255) * kSelCopies + (lane & (kSelCopies - 1))], 1u);
     }
     __syncthreads();
     {                                           // four threads to a counter, four copies each
@@ -108,18 +120,37 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(EvictArgs a) 
     prefix = prefix << 8 | digit;
     need -= (int)above;
   }
-  // ---- every key above prefix, and the first `need` that equal it, in order ----
-  const int per = ((m + kSelWaves - 1) / kSelWaves + 63) / 64 * 64;
-  const int j0 = min(wave * per, m), j1 = min(j0 + per, m);
-  int gt = 0, eq = 0;
-  for (int j = j0 + lane; j < j0 + per; j += 64) {
-    const uint32_t u = j < j1 ? key_at(j) : 0u;
-    gt += __popcll(__ballot(j < j1 && u > prefix));
-    eq += __popcll(__ballot(j < j1 && u == prefix));
+  // ---- every key above prefix, and the first `need` that equal it, in order: a wave takes consecutive quads, a lane one ----
+  const int per = ((quads + kSelWaves - 1) / kSelWaves + 63) / 64 * 64;
+  const int q0 = wave * per, q1 = min(q0 + per, quads);
+  // how many of the quad are above and equal
+  auto count = [&](int q, u32x4& u, int& gt, int& eq) __attribute__((always_inline)) {
+    gt = eq = 0;
+    u = u32x4{0, 0, 0, 0};
+    if (q < q1) {
+      u = keys_at(q);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        gt += 4 * q + x < m && u[x] > prefix;
+        eq += 4 * q + x < m && u[x] == prefix;
+      }
+    }
+  };
+  // sum over the lanes selected, of numbers of 0 .. 4
+  auto over = [&](int v, unsigned long long lanes) __attribute__((always_inline)) -> int {
+    return __popcll(__ballot(v & 1) & lanes) + 2 * __popcll(__ballot(v & 2) & lanes) + 4 * __popcll(__ballot(v & 4) & lanes);
+  };
+  int gt_all = 0, eq_all = 0;
+  for (int q = q0 + lane; q < q0 + per; q += 64) {
+    u32x4 u;
+    int gt, eq;
+    count(q, u, gt, eq);
+    gt_all += over(gt, ~0ull);
+    eq_all += over(eq, ~0ull);
   }
   if (lane == 0) {
-    sm_gt[wave] = gt;
-    sm_eq[wave] = eq;
+    sm_gt[wave] = gt_all;
+    sm_eq[wave] = eq_all;
   }
   __syncthreads();
   int gt0 = 0, eq0 = 0;
@@ -127,15 +158,21 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(EvictArgs a) 
     gt0 += sm_gt[w];
     eq0 += sm_eq[w];
   }
-  for (int j = j0 + lane; j < j0 + per; j += 64) {
-    const uint32_t u = j < j1 ? key_at(j) : 0u;
-    const unsigned long long g = __ballot(j < j1 && u > prefix), q = __ballot(j < j1 && u == prefix);
+  for (int q = q0 + lane; q < q0 + per; q += 64) {
+    u32x4 u;
+    int gt, eq;
+    count(q, u, gt, eq);
     const unsigned long long below = (1ull << lane) - 1;
-    const int my_eq = eq0 + __popcll(q & below), my_gt = gt0 + __popcll(g & below);
-    const bool is_gt = (g >> lane) & 1, is_eq = (q >> lane) & 1;
-    if (is_gt || (is_eq && my_eq < need)) kept[my_gt + min(my_eq, need)] = j;
-    gt0 += __popcll(g);
-    eq0 += __popcll(q);
+    int my_gt = gt0 + over(gt, below), my_eq = eq0 + over(eq, below);
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const bool is_gt = q < q1 && 4 * q + x < m && u[x] > prefix, is_eq = q < q1 && 4 * q + x < m && u[x] == prefix;
+      if (is_gt || (is_eq && my_eq < need)) kept[my_gt + min(my_eq, need)] = 4 * q + x;
+      my_gt += is_gt;
+      my_eq += is_eq;
+    }
+    gt0 += over(gt, ~0ull);
+    eq0 += over(eq, ~0ull);
   }
 }
 
@@ -143,7 +180,6 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(EvictArgs a) 
 // column parts of K and V, 2 * parts the weights; otherwise y takes a share of the rows with everything that belongs to them.
 template <bool IN_ORDER>
 __global__ __launch_bounds__(IN_ORDER ? 1024 : kMoveThreads) void evict_move_kernel(EvictArgs a, int parts) {
-  typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
   const int h = blockIdx.x, part = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
   const int n = min(max(a.src.lens[b], 0), a.src.cap), m = min(min(n, a.budget), a.dst.cap);
   if (part == 0 && h == 0 && tid == 0) a.lens_out[b] = m;
@@ -211,7 +247,7 @@ __global__ __launch_bounds__(IN_ORDER ? 1024 : kMoveThreads) void evict_move_ker
 
 hipError_t launch_evict(const EvictArgs& a, hipStream_t s) {
   const int most = std::min(std::max(a.src.cap - a.recent, 1), kSelKeys);
-  const size_t smem = (size_t)most * sizeof(uint32_t);
+  const size_t smem = (size_t)(most + 3) / 4 * 16;
   hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(evict_select_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(evict_select_kernel, dim3(a.Hkv, a.B), dim3(kSelThreads), smem, s, a);

@@ -419,7 +419,7 @@ hipError_t launch(WeightsArgs a, hipStream_t s) {
     a.p.R = 0;
     a.p.G = a.Hq / a.Hkv;
     a.p.slots_log2 = 0;
-    while ((1 << a.p.slots_log2) * a.Hkv < 1024) ++a.p.slots_log2;
+    while ((1 << a.p.slots_log2) * a.Hkv < 2048) ++a.p.slots_log2;
     a.p.least = 8;
     a.p.max_splits = std::max(1, (a.c.cap + 255) / 256);
     const int items = (int)std::min((long long)a.r.B + (1 << a.p.slots_log2), (long long)a.r.B * a.p.max_splits);
