@@ -220,6 +220,8 @@ hipError_t launch_rows(const ChunkArgs& a, const RowPlan& r, hipStream_t s) {
   return hipGetLastError();
 }
 
+constexpr double kBlockLeastFlops = 1e9;
+
 // Rows per workgroup, ranges and the bounds of both, from what the host knows: B requests, `total` new tokens of which no request
 // has more than max_q, caches of up to S tokens.
 RowPlan row_plan(int B, int S, int Hq, int Hkv, int D, int dtype, int total, int max_q) {
@@ -227,21 +229,27 @@ RowPlan row_plan(int B, int S, int Hq, int Hkv, int D, int dtype, int total, int
   const int G = Hq / Hkv, blocks = (S + 31) / 32;
   const bool bf16 = dtype == SEKA_BF16;
   const long long rows = (long long)std::min(max_q, total) * G;
-  r.rows16 = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-  r.p.R = 16 * r.rows16;
   r.p.G = G;
+  r.p.least = bf16 ? 8 : 4;                // 256 tokens, 128: a block of every wave of eight
+  const long long ranges = std::max(1, std::min(kMaxRanges, (blocks + r.p.least - 1) / r.p.least));
+  auto chunks_of = [&](int R) { return std::min(((long long)total * G) / R + B, 0x3fffffffll); };
+  // fp32 chunks that are long enough, and enough of them, for waves with rows of their own that share their keys
+  r.block = !bf16 && rows > 64 && 4.0 * D * total * Hq * S > kBlockLeastFlops;
+  // as many tiles of 16 rows as there are, up to four, but no more than leave two workgroups for every compute unit
+  r.rows16 = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+  while (!r.block && r.rows16 > 1 && chunks_of(16 * r.rows16) * ranges * Hkv < 512) r.rows16 /= 2;
+  r.p.R = r.block ? kBlockRows : 16 * r.rows16;
   r.rows = (int)std::min(rows, (long long)r.p.R);
-  const long long chunks = std::min(((long long)total * G) / r.p.R + B, 0x3fffffffll);
+  const long long chunks = chunks_of(r.p.R);
   // eight waves to a workgroup where the keys are few: a range is then half as long a chain
-  const bool few = r.rows16 <= 2 && chunks * blocks * Hkv <= 256 * 8 * 2;
+  const bool few = !r.block && r.rows16 <= 2 && chunks * blocks * Hkv <= 256 * 8 * 2;
   r.waves = few ? 8 : 4;
   // two workgroups of four waves to a compute unit, about, or one of eight
   r.p.slots_log2 = 0;
   while ((1 << r.p.slots_log2) * Hkv < (few ? 256 : 512)) ++r.p.slots_log2;
-  r.p.least = bf16 ? 8 : 4;                // 256 tokens, 128: a block of every wave of eight
-  r.p.max_splits = std::max(1, std::min(kMaxRanges, (blocks + r.p.least - 1) / r.p.least));
-  // and no second kernel where a wave has four blocks of bf16 keys, or eight of fp32 ones, at most
-  if (few && S <= 1024) r.p.max_splits = 1;
+  r.p.max_splits = (int)ranges;
+  // and no second kernel where a wave has no more than four blocks (fp32, 777 tokens in one range: 14.5 us, in ranges 9.9)
+  if (few && S <= (bf16 ? 1024 : 512)) r.p.max_splits = 1;
   r.p.streams = (long long)(300e6 / (2.0 * 32 * Hkv * D * (bf16 ? 2 : 4)));
   // sum over chunks of ceil(blocks / L) <= T / L + chunks with T / L <= slots, and no more than every chunk in all its ranges
   r.items = (int)std::min(chunks + (1 << r.p.slots_log2), chunks * r.p.max_splits);

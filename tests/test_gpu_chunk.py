@@ -24,8 +24,8 @@ def check(seka, x, what, **kw):
     used = int(x.cu[-1])
     ref = orc.chunk_attention(x.Q, x.K, x.V, x.table, x.lens, x.cu, scale=kw.get("scale") or None)
     ref = (ref[0][:used], ref[1][:, :used], ref[2][:used], ref[3][:, :used])
-    # chunks that are long enough for it: also with the kernel of long caches, which a bound on the cached tokens asks for
-    far = x.dtype == "bf16" and max(x.new) * x.Hq // x.Hkv > 64 and "max_len" not in kw
+    # chunks that are long enough for it: also with the kernel of long chunks, which a bound on the cached tokens asks for
+    far = max(x.new) * x.Hq // x.Hkv > 64 and "max_len" not in kw
     for more in ({}, dict(max_len=min(100000, (1 << 31) // (x.Hq * x.D) - 1))) if far else ({},):
         O, L = run(seka, x, **kw, **more)
         P.check_attention(P.f64(O)[:used], P.f64(L)[:, :used] if L is not None else None, ref, x.dtype, f"{what} {more}", lse=L is not None)
