@@ -21,7 +21,7 @@ typedef __attribute__((address_space(3))) s16x4* row_lds_s16x4_ptr;
 typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
 
 template <int D, int RT, int NW>
-__global__ __launch_bounds__(64 * NW, RT == 4 && D == 128 ? 1 : 2) void chunk_rows_bf16_kernel(ChunkArgs a) {
+__global__ __launch_bounds__(64 * NW, 2) void chunk_rows_bf16_kernel(ChunkArgs a) {
   constexpr int BK = 32, R = 16 * RT;
   // LDS row strides (elements): 16 rows of K at one 16-byte column, and 16 rows x 32 bytes of V, spread over all banks
   constexpr int LDK = D + 8, LDV = D + 16, OLD = D + 4;
@@ -209,7 +209,7 @@ void launch_rows(const ChunkArgs& a, const RowPlan& r, hipStream_t s) {
   const dim3 grid(r.items, a.Hkv), block(64 * NW);
   if (r.rows16 == 1) hipLaunchKernelGGL((chunk_rows_bf16_kernel<D, 1, NW>), grid, block, 0, s, a);
   else if (r.rows16 == 2) hipLaunchKernelGGL((chunk_rows_bf16_kernel<D, 2, NW>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((chunk_rows_bf16_kernel<D, 4, 4>), grid, dim3(256), 0, s, a);
+  else if constexpr (D == 64) hipLaunchKernelGGL((chunk_rows_bf16_kernel<D, 4, 4>), grid, dim3(256), 0, s, a);
 }
 
 template <int D>
@@ -235,14 +235,15 @@ RowPlan row_plan(int B, int S, int Hq, int Hkv, int D, int dtype, int total, int
   auto chunks_of = [&](int R) { return std::min(((long long)total * G) / R + B, 0x3fffffffll); };
   // fp32 chunks that are long enough, and enough of them, for waves with rows of their own that share their keys
   r.block = !bf16 && rows > 64 && 4.0 * D * total * Hq * S > kBlockLeastFlops;
-  // as many tiles of 16 rows as there are, up to four, but no more than leave two workgroups for every compute unit
-  r.rows16 = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+  // as many tiles of 16 rows as there are, up to two (D = 64: four), but no more than leave two workgroups for every compute unit.  Four at
+  // D = 128 need the registers of two waves: 10 new tokens over 24967, 32 / 8 heads, 60.1 us, in two chunks of two tiles 32.5.
+  r.rows16 = rows <= 16 ? 1 : rows <= 32 || D == 128 ? 2 : 4;
   while (!r.block && r.rows16 > 1 && chunks_of(16 * r.rows16) * ranges * Hkv < 512) r.rows16 /= 2;
   r.p.R = r.block ? kBlockRows : 16 * r.rows16;
   r.rows = (int)std::min(rows, (long long)r.p.R);
   const long long chunks = chunks_of(r.p.R);
   // eight waves to a workgroup where the keys are few: a range is then half as long a chain
-  const bool few = !r.block && r.rows16 <= 2 && chunks * blocks * Hkv <= 256 * 8 * 2;
+  const bool few = !r.block && r.rows16 <= 2 && chunks * blocks * Hkv <= 256 * 8 * 2 && chunks * Hkv <= 256;
   r.waves = few ? 8 : 4;
   // two workgroups of four waves to a compute unit, about, or one of eight
   r.p.slots_log2 = 0;
@@ -266,14 +267,16 @@ int compute_units() {
   });
 }
 
-constexpr double kPipeLeastFlops = 3e9;
+// Products of a call's rows with S keys each, in flops, from which on long chunks go to the pipelined kernel.  us, kernel of few rows / pipelined, 32 / 8
+// heads: 4.3e9 n=128 S=2048 27.7 / 34.1, n=512 S=512 25.0 / 28.1; 24 / 8 heads, about 4e9, three of up to 185 over 1077 42.1 / 29.1; 8.6e9 four of up to 64 over 4096 42.5 / 32.8; 1.6e10
+// n=1000 S=1000 52.4 / 37.9; 3.4e10 n=512 S=4096 103 / 53.5.
+constexpr double kPipeLeastFlops = 3.5e9;
 
 // Whether a call's chunks go to the pipelined kernel, and how: bf16, more rows per KV head than four tiles of 16, and a cache
 // whose page numbers fit beside the tiles in LDS (4 bytes for every page of S tokens).
 bool pipe_plan(int S, int Hq, int Hkv, int D, int dtype, int shift, int total, int max_q, PipeChunkPlan* out) {
   const int G = Hq / Hkv;
   if (dtype != SEKA_BF16 || (long long)std::min(max_q, total) * G <= 64) return false;
-  // little work goes to the kernel of few rows all the same: this one takes some 30 us for any
   if (4.0 * D * total * Hq * S <= kPipeLeastFlops) return false;
   out->hpw = G % 4 == 0 ? 4 : G % 7 == 0 ? 7 : G % 2 == 0 ? 2 : 1;
   out->rbw = out->hpw == 7 ? 1 : 8 / out->hpw;

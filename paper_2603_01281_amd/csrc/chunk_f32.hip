@@ -339,7 +339,7 @@ void launch_rows(const ChunkArgs& a, const RowPlan& r, hipStream_t s) {
   const dim3 grid(r.items, a.Hkv), block(64 * NW);
   if (r.rows16 == 1) hipLaunchKernelGGL((chunk_rows_f32_kernel<D, 1, NW>), grid, block, 0, s, a);
   else if (r.rows16 == 2) hipLaunchKernelGGL((chunk_rows_f32_kernel<D, 2, NW>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((chunk_rows_f32_kernel<D, 4, 4>), grid, dim3(256), 0, s, a);
+  else if constexpr (D == 64) hipLaunchKernelGGL((chunk_rows_f32_kernel<D, 4, 4>), grid, dim3(256), 0, s, a);
 }
 
 template <int D>

@@ -15,8 +15,10 @@
 namespace seka {
 
 constexpr int kPipeOver = 10;            // half tiles that a block costs beside its keys (stamps of the dense kernel: 4.7 tiles)
-constexpr int kPipeSnap = 6;             // no piece of fewer tiles
-constexpr int kPipeLeastLog2 = 5;        // half tiles of a workgroup, at least (log2)
+// No piece of fewer tiles; half tiles of a workgroup, at least (log2).  us, 32 / 8 heads, 6 tiles and 32 halves / 2 and 8: one chunk of 512 over 512
+// 39.0 / 28.1, 128 over 2048 42.1 / 34.1, four of up to 64 over 4096 43.4 / 32.8, 512 over 4096 57.4 / 53.5.
+constexpr int kPipeSnap = 2;
+constexpr int kPipeLeastLog2 = 3;
 
 struct PipeCut {
   int b, k, t;           // request, block, tile
