@@ -386,6 +386,8 @@ seka_status seka_cache_append(const void* K, const void* V, const void* Q, void*
  * sh->S      the most cached tokens of a request (it sizes the launch; longer caches are cut to their first S tokens).
  * max_q      the longest chunk, 1 .. S.
  * A token that sees no key (lens[b] smaller than n) gets O = 0 and lse = -inf.  Keys and values behind lens[b] are never read.
+ * A cached value (V) that is not finite reaches all of its request's new tokens, also those that do not see it.
+ * lse is that of the probabilities before their rounding to bf16, good to fp32 whatever the lengths.
  * workspace  dev scratch of at least seka_chunk_workspace_bytes(...) bytes, 16-byte aligned; contents on return are
  *            unspecified; calls sharing it must be ordered by their stream.
  * Deterministic for given arguments and lengths.  A token's bits may differ with the batch it is in (its keys are then cut into
@@ -399,7 +401,8 @@ seka_status seka_attention_chunk(const void* Q, void* O, float* lse, const seka_
 /*
  * seka_attention_weights — the attention that every cached token gets, summed over a chunk's queries and the heads of its group:
  *   W[b,h,j] = decay * W_in[b,h,j] + sum_g sum_i exp(scale q_{i,g} . k_j - lse_{i,g}),  the last `window` new tokens i that see j
- * for all cached tokens j < lens[b]; other slots are left untouched.
+ * for all cached tokens j < lens[b]; other slots are left untouched.  No page may belong to two requests of the call (a prefix that
+ * requests share for attention has one weight per slot, and each of them would write it).
  *
  * Q          dev [total_tokens,Hq,D] as given to seka_attention_chunk;  lse dev [Hq,total_tokens], its result.
  * cache->W   dev (written; required);  W_in dev, same layout, may be cache->W itself, or NULL: the sums alone.

@@ -83,6 +83,20 @@ __device__ __forceinline__ bool plan_item(const ChunkRows& r, const PagedCache& 
       blocks = (e.len + 31) >> 5;
     }
   };
+  if (r.B == 1) {                        // nothing to add up over requests
+    out.b = 0;
+    out.e = chunk_extent(r, c, 0);
+    chunks = p.R ? (int)(((unsigned)out.e.n * (unsigned)p.G + p.R - 1) / (unsigned)p.R) : out.e.len > 0;
+    blocks = (out.e.len + 31) >> 5;
+    const unsigned long long T = (unsigned long long)chunks * (unsigned)blocks;
+    const unsigned long long per = (T + (1ull << p.slots_log2) - 1) >> p.slots_log2;
+    const int L = (int)max((unsigned long long)p.least, min(per, 0x7fffffffull));
+    out.streams = T > (unsigned long long)p.streams;
+    out.splits = max(1, min((blocks + L - 1) / L, p.max_splits));
+    out.rc = item / out.splits;
+    out.split = item - out.rc * out.splits;
+    return out.rc < chunks;
+  }
   unsigned long long T = 0;
   for (int b0 = 0; b0 < r.B; b0 += 64) {
     look(b0);
