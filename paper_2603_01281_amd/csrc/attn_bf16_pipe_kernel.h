@@ -207,10 +207,10 @@ constexpr int pipe_element_at(int m, int mfmas) {
 
 struct PipeDense {};             // the arguments of pages where there are none
 
-// New tokens that see no key (more of them than cached tokens): the requests item, item + width, .. of a head chunk.
-template <int D, int HPW>
-__device__ __forceinline__ void pipe_rows_without_keys(const ChunkArgs& pg, int item, int hc) {
-  const int lane = threadIdx.x & 63;
+// New tokens that see no key (more of them than cached tokens): the requests item, item + width, .. of a KV head.
+template <int D>
+__device__ __forceinline__ void pipe_rows_without_keys(const ChunkArgs& pg, int item, int h) {
+  const int lane = threadIdx.x & 63, G = pg.Hq / pg.Hkv;
   for (int b0 = 0; b0 < pg.r.B; b0 += 64) {
     ChunkExtent e = {0, 0, 0};
     const int mine = b0 + lane;
@@ -219,12 +219,12 @@ __device__ __forceinline__ void pipe_rows_without_keys(const ChunkArgs& pg, int 
     for (; todo; todo &= todo - 1) {       // rare: lengths that do not count the new tokens
       const int l = __builtin_ctzll(todo);
       const int rows = __shfl(e.n - e.len, l), row0 = __shfl(e.row0, l);
-      for (int x = threadIdx.x; x < rows * HPW * (D / 8); x += blockDim.x) {
-        const size_t row = (size_t)(row0 + x / (HPW * (D / 8))) * pg.Hq + hc * HPW;
-        reinterpret_cast<uint4*>(static_cast<uint16_t*>(pg.O) + row * D)[x % (HPW * (D / 8))] = make_uint4(0, 0, 0, 0);
+      for (int x = threadIdx.x; x < rows * G * (D / 8); x += blockDim.x) {
+        const size_t row = (size_t)(row0 + x / (G * (D / 8))) * pg.Hq + h * G;
+        reinterpret_cast<uint4*>(static_cast<uint16_t*>(pg.O) + row * D)[x % (G * (D / 8))] = make_uint4(0, 0, 0, 0);
       }
       if (pg.lse)
-        for (int x = threadIdx.x; x < rows * HPW; x += blockDim.x) pg.lse[(size_t)(hc * HPW + x % HPW) * pg.r.total + row0 + x / HPW] = -INFINITY;
+        for (int x = threadIdx.x; x < rows * G; x += blockDim.x) pg.lse[(size_t)(h * G + x % G) * pg.r.total + row0 + x / G] = -INFINITY;
     }
   }
 }
@@ -232,17 +232,19 @@ __device__ __forceinline__ void pipe_rows_without_keys(const ChunkArgs& pg, int 
 template <class PIECES, class PG>
 __device__ __forceinline__ PIECES pipe_pieces_of(const PG& pg, int item) {
   if constexpr (std::is_same_v<PG, PipeDense>) return PIECES{};
-  else return PIECES(pg.r, pg.c, pg.width, item);
+  else return PIECES(pg.r, pg.c, pg.width, pg.Hq / pg.Hkv, item);
 }
 
 // HPW heads x RBW row groups = waves per workgroup; every wave owns 32 consecutive query rows, two row tiles of 16.
 // NKR: rank of the concatenated basis in blocks of 32 columns (compile-time so that the edit is straight-line code).
 // PAGED: keys and values in pages (seka_attention_chunk, pg); a workgroup's pieces come from chunk_plan.h.  A piece is worked on as if
-// its first key were key 0: positions of rows and the number of keys are relative to it.
+// its first key were key 0: positions of rows and the number of keys are relative to it.  HPW = 1; a wave's 32 rows are those of
+// a few positions and all heads of the KV head's group (chunk_plan.h), qw the 32 positions that they lie in.
 template <int D, int HPW, int RBW, bool STEER, int NKR, class PG>
 __device__ __forceinline__ void attention_bf16_pipe_body(const AttnArgs& a, const SteerArgs& st, const PG& pg) {
   constexpr bool PAGED = !std::is_same_v<PG, PipeDense>;
   static_assert(!(PAGED && STEER), "keys in pages are edited before they are stored");
+  static_assert(!PAGED || (HPW == 1 && RBW == kPipeWaves), "rows of the plan");
   static_assert(D == 64 || D == 128, "head dimensions of the tile layouts");
   constexpr int NW = HPW * RBW;
   constexpr int NT = 64 * NW;
@@ -278,7 +280,7 @@ __device__ __forceinline__ void attention_bf16_pipe_body(const AttnArgs& a, cons
 
   const int Scap = a.S;                      // tokens per prompt in memory (strides, launch grid)
   const int G = a.Hq / a.Hkv;
-  const int nHC = a.Hq / HPW;
+  const int nHC = PAGED ? a.Hkv : a.Hq / HPW;
   // A workgroup handles several blocks of query rows of one (batch, head group), one after the other.  A prompt's
   // blocks, latest (longest) first, are dealt to its W workgroups back and forth: slot 0 .. W-1, then W-1 .. 0 and so
   // on.  Two deals give every slot the same number of key tiles, so there is no imbalance from causality; the
@@ -290,23 +292,25 @@ __device__ __forceinline__ void attention_bf16_pipe_body(const AttnArgs& a, cons
   const int hc = (int)(blockIdx.x % nHC);
   const int item = (int)(blockIdx.x / nHC);
   const int hq0 = hc * HPW;
-  const int h = hq0 / G;
+  const int h = PAGED ? hc : hq0 / G;
   int b, slot, W = a.width;
   size_t tok0;                               // first token of this prompt in the tensors
   int S;                                     // this prompt's length: rows and keys beyond it do not exist
   int nblocks, qb;
-  using Pieces = std::conditional_t<PAGED, PipePieces<BQ>, PipeDense>;
+  using Pieces = std::conditional_t<PAGED, PipePieces, PipeDense>;
   [[maybe_unused]] Pieces pieces = pipe_pieces_of<Pieces>(pg, item);
   [[maybe_unused]] PipePiece piece = {};
   [[maybe_unused]] int key0 = 0;             // the piece's first key
-  [[maybe_unused]] int first_row = 0;        // position of the block of rows, and of the request's first new token, relative to key0
+  [[maybe_unused]] int first_row = 0;        // position of row 0, and of the request's first new token, relative to key0
   [[maybe_unused]] int first_new = 0;
+  [[maybe_unused]] int first_wave = 0;       // of the block, in waves from row 0
   auto take_piece = [&]() __attribute__((always_inline)) {
     if constexpr (PAGED) {
       key0 = 64 * piece.t0;
       S = piece.e.len - key0;
       const int ctx = piece.e.len - piece.e.n;
-      first_row = PipePlan<BQ>::first_row(piece.e) + piece.k * BQ - key0;
+      first_row = PipePlan::first_row(piece.e) - key0;
+      first_wave = pieces.p.first_wave(piece.e) + kPipeWaves * piece.k;
       first_new = max(ctx, 0) - key0;
       tok0 = (size_t)((long long)piece.e.row0 - ctx + key0);       // row of the tensors of position 0
       b = piece.b;
@@ -315,7 +319,7 @@ __device__ __forceinline__ void attention_bf16_pipe_body(const AttnArgs& a, cons
   if constexpr (PAGED) {
     slot = nblocks = qb = 0;
     if (hc == 0 && threadIdx.x == 0) pg.cuts[item] = make_int4(pieces.start.b, pieces.start.k, pieces.start.t, 0);
-    pipe_rows_without_keys<D, HPW>(pg, item, hc);
+    pipe_rows_without_keys<D>(pg, item, hc);
     if (!pieces.next(piece)) return;         // workgroup-uniform, before any barrier
     take_piece();
   } else {
@@ -338,8 +342,24 @@ __device__ __forceinline__ void attention_bf16_pipe_body(const AttnArgs& a, cons
   const int hq = hq0 + wave / RBW;
   // Waves w and w + 4 share a SIMD: their row blocks are chosen to end on different tiles or halves of a tile.
   const int rb = RBW == 1 ? 0 : RBW == 2 ? (wave ^ (wave >> 2)) & 1 : RBW == 4 ? (wave & 3) ^ (wave >> 2 ? 3 : 0) : wave < 4 ? wave : 11 - wave;
-  int qw = PAGED ? first_row + WR * rb : qb * BQ + WR * rb;    // first query row of this wave
-  int qi0 = qw + l16;                      // this lane's query row in row tile 0 (tile 1: + 16)
+  // PAGED: row x of this wave: head and position
+  auto row_of = [&](int x) __attribute__((always_inline)) {
+    const unsigned row = (unsigned)(WR * (first_wave + rb) + x), at = row / (unsigned)G;
+    return int2{(int)(row - at * G), first_row + (int)at};
+  };
+  int qw, qi0, qi1;                        // first query row of this wave; this lane's in row tiles 0 and 1
+  auto wave_rows = [&]() __attribute__((always_inline)) {
+    if constexpr (PAGED) {
+      qw = first_row + WR * (int)((unsigned)(first_wave + rb) / (unsigned)G);
+      qi0 = row_of(l16).y;
+      qi1 = row_of(16 + l16).y;
+    } else {
+      qw = qb * BQ + WR * rb;
+      qi0 = qw + l16;
+      qi1 = qi0 + 16;
+    }
+  };
+  wave_rows();
 
   const float gain = STEER ? st.gain[h] : 0.f;
   const float kscale = STEER ? st.kscale[h] : 1.f;
@@ -525,9 +545,14 @@ __device__ __forceinline__ void attention_bf16_pipe_body(const AttnArgs& a, cons
     // order, 32 rows x 32 bytes per load, the address unit took 3 cycles per row: 6000 cycles per block.)
 #pragma unroll
     for (int i = 0; i < 2 * KS; ++i) {    // rows past the end read row 0 (finite data, results never stored):
-      const int qi = qw + 8 * (i & 3) + (lane >> 3);                                          // no branch, no wait here
+      int qi = qw + 8 * (i & 3) + (lane >> 3), head = hq;                                     // no branch, no wait here
+      if constexpr (PAGED) {
+        const int2 at = row_of(8 * (i & 3) + (lane >> 3));
+        qi = at.y;
+        head = h * G + at.x;
+      }
       const bool there = qi < S && (!PAGED || qi >= first_new);
-      const uint16_t* qp = Qg + ((tok0 + (there ? qi : PAGED ? first_new : 0)) * a.Hq + hq) * D + 64 * (i >> 2) + 8 * (lane & 7);
+      const uint16_t* qp = Qg + ((tok0 + (there ? qi : PAGED ? first_new : 0)) * a.Hq + head) * D + 64 * (i >> 2) + 8 * (lane & 7);
       qf[i] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(qp));
     }
   };
@@ -960,7 +985,7 @@ __device__ __forceinline__ void attention_bf16_pipe_body(const AttnArgs& a, cons
       for (int rt = 0; rt < 2; ++rt)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          if (jbase + 16 * kt + i > qi0 + 16 * rt) sv[kt][rt][i] = -INFINITY;
+          if (jbase + 16 * kt + i > (PAGED ? (rt ? qi1 : qi0) : qi0 + 16 * rt)) sv[kt][rt][i] = -INFINITY;
   };
   // Row maximum (of s * c2) over one 32-key block, all lanes of the row.
   auto block_max = [&](int rt, const f32x4 (&sv)[2][2]) __attribute__((always_inline)) -> float {
@@ -1036,7 +1061,7 @@ __device__ __forceinline__ void attention_bf16_pipe_body(const AttnArgs& a, cons
     }
   };
 
-  const bool wave_rows_exist = qw < S && (!PAGED || qw >= 0);      // PAGED: a piece may start behind the last key that a wave's rows see
+  const bool wave_rows_exist = PAGED ? qw >= 0 && row_of(0).y < S : qw < S;      // PAGED: a piece may start behind the last key that a wave's rows see
   const int tw_last = wave_rows_exist ? min(ntiles - 1, (qw + WR - 1) / BK) : -1;   // last tile this wave computes on
 
   // ---- prologue: wait for the first tiles, edit K(0) and K(1), first block of S^T ----
@@ -1436,8 +1461,7 @@ __device__ __forceinline__ void attention_bf16_pipe_body(const AttnArgs& a, cons
     if (more) {
       dma_barrier();
       qb = nblocks - 1 - dealt;
-      qw = qb * BQ + WR * rb;
-      qi0 = qw + l16;
+      wave_rows();
       last_key = min(S, qb * BQ + BQ) - 1;
       ntiles = last_key / BK + 1;
       begin_block();
@@ -1458,7 +1482,7 @@ __device__ __forceinline__ void attention_bf16_pipe_body(const AttnArgs& a, cons
   if (joined) {
     // a part of the block's keys: outputs as they are, reference exponent and sum, for the kernel that joins them
     float* part = nullptr;
-    if constexpr (PAGED) part = pg.part + (((size_t)pieces.slot(piece) * nHC + hc) * (HPW * BQ) + (wave / RBW) * BQ + WR * rb) * (D + 4);
+    if constexpr (PAGED) part = pg.part + (((size_t)pieces.slot(piece) * nHC + hc) * BQ + WR * rb) * (D + 4);
 #pragma unroll
     for (int rt = 0; rt < 2; ++rt) {
       float* const row = part + (16 * rt + (ln & 15)) * (D + 4);
@@ -1485,17 +1509,26 @@ __device__ __forceinline__ void attention_bf16_pipe_body(const AttnArgs& a, cons
     asm volatile("" ::: "memory");
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int qi = qw_out + 8 * i + (ln >> 3);
+      int qi = qw_out + 8 * i + (ln >> 3), head = hq;
+      if constexpr (PAGED) {
+        const int2 at = row_of(8 * i + (ln >> 3));
+        qi = at.y;
+        head = h * G + at.x;
+      }
       const u32x4 line = *stg_line(ln, i);
-      if (qi < S && (!PAGED || qi >= first_new)) *reinterpret_cast<u32x4*>(Og + ((tok0 + qi) * a.Hq + hq) * D + 64 * half + 8 * (ln & 7)) = line;
+      if (qi < S && (!PAGED || qi >= first_new)) *reinterpret_cast<u32x4*>(Og + ((tok0 + qi) * a.Hq + head) * D + 64 * half + 8 * (ln & 7)) = line;
     }
     asm volatile("" ::: "memory");
   }
   // m_run is the reference exponent in units of s * scale * log2(e); the sums are relative to it
   if (a.lse && grp < 2) {                  // lane group rt writes row tile rt
-    const int qi = qw_out + lane;
+    int qi = qw_out + lane;
     size_t at;
-    if constexpr (PAGED) at = (size_t)hq * pg.r.total + (tok0 + qi);
+    if constexpr (PAGED) {
+      const int2 row = row_of(lane);
+      qi = row.y;
+      at = (size_t)(h * G + row.x) * pg.r.total + (tok0 + qi);
+    }
     else at = lse_index(a, b, hq, tok0, qi);
     if (qi < S && (!PAGED || qi >= first_new)) a.lse[at] = (grp ? m_run[1] : m_run[0]) * 0.6931471805599453f + logf(grp ? lacc[1][0] : lacc[0][0]);
   }
@@ -1504,8 +1537,7 @@ __device__ __forceinline__ void attention_bf16_pipe_body(const AttnArgs& a, cons
     if (!pieces.next(piece)) break;
     dma_barrier();                         // the rings and the list of pages are free
     take_piece();
-    qw = first_row + WR * rb;
-    qi0 = qw + l16;
+    wave_rows();
     ntiles = piece.t1 - piece.t0;
     begin_block();
   } else {

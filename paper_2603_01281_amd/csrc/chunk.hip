@@ -115,6 +115,7 @@ __global__ __launch_bounds__(64 * NW, 2) void chunk_rows_bf16_kernel(ChunkArgs a
     win.load(a.c, it.b, kb, k1);
     fetch(nt, kb);
   }
+  row_arrived(qf);
   for (; kb < k1; kb += NW * BK) {
     // (a wave's LDS operations execute in program order; the fences are for the compiler)
 #pragma unroll
@@ -249,8 +250,9 @@ RowPlan row_plan(int B, int S, int Hq, int Hkv, int D, int dtype, int total, int
   r.p.slots_log2 = 0;
   while ((1 << r.p.slots_log2) * Hkv < (few ? 256 : 512)) ++r.p.slots_log2;
   r.p.max_splits = (int)ranges;
-  // and no second kernel where a wave has no more than four blocks (fp32, 777 tokens in one range: 14.5 us, in ranges 9.9)
-  if (few && S <= (bf16 ? 1024 : 512)) r.p.max_splits = 1;
+  // and no second kernel where a wave has no more than four blocks, eight of four waves (bf16, 37 requests of up to 24 over 526, 32 / 4 heads, D = 64:
+  // 27.4 us in ranges, 12.8 in one each; fp32, 777 tokens in one range: 14.5 us, in ranges 9.9)
+  if (bf16 ? S <= 1024 : few && S <= 512) r.p.max_splits = 1;
   r.p.streams = (long long)(300e6 / (2.0 * 32 * Hkv * D * (bf16 ? 2 : 4)));
   // sum over chunks of ceil(blocks / L) <= T / L + chunks with T / L <= slots, and no more than every chunk in all its ranges
   r.items = (int)std::min(chunks + (1 << r.p.slots_log2), chunks * r.p.max_splits);
@@ -278,12 +280,9 @@ bool pipe_plan(int S, int Hq, int Hkv, int D, int dtype, int shift, int total, i
   const int G = Hq / Hkv;
   if (dtype != SEKA_BF16 || (long long)std::min(max_q, total) * G <= 64) return false;
   if (4.0 * D * total * Hq * S <= kPipeLeastFlops) return false;
-  out->hpw = G % 4 == 0 ? 4 : G % 7 == 0 ? 7 : G % 2 == 0 ? 2 : 1;
-  out->rbw = out->hpw == 7 ? 1 : 8 / out->hpw;
-  const int nHC = Hq / out->hpw, cus = compute_units();
-  out->width = std::max(1, cus / nHC);
-  out->smem = attention_bf16_pipe_smem_bytes(D, 0, false, 1, out->hpw * out->rbw) + (((size_t)S >> shift) + 2) * sizeof(int);
-  out->cuts = (size_t)2 * out->width * Hq * (32 * out->rbw) * (D + 4) * sizeof(float);      // behind the states, two per workgroup
+  out->width = std::max(1, compute_units() / Hkv);
+  out->smem = attention_bf16_pipe_smem_bytes(D, 0, false, 1, kPipeWaves) + (((size_t)S >> shift) + 2) * sizeof(int);
+  out->cuts = (size_t)2 * out->width * Hkv * kPipeRows * (D + 4) * sizeof(float);      // behind the states, two per workgroup
   out->workspace = out->cuts + (size_t)out->width * sizeof(int4);
   return out->smem <= 160 * 1024;
 }

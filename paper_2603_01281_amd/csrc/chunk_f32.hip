@@ -97,8 +97,11 @@ __global__ __launch_bounds__(64 * NW, RT == 4 ? 1 : 2) void chunk_rows_f32_kerne
     fetch_k(kb);
     fetch_v(kb);
   }
-  for (; kb < k1; kb += TURN) {
-    const bool more = kb + TURN < k1;
+  row_arrived(qv);
+  // MORE: with keys behind these.  (A branch in the loop instead, and the waits are for what both of its sides have in flight, the next keys too:
+  // 6 requests at one token over 29278, 32 / 32 heads, 598 us, without 553.)
+  auto step = [&](auto more_c) __attribute__((always_inline)) {
+    constexpr bool MORE = decltype(more_c)::value;
     f32x4 t[RT];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
@@ -115,9 +118,10 @@ __global__ __launch_bounds__(64 * NW, RT == 4 ? 1 : 2) void chunk_rows_f32_kerne
         for (int c = 0; c < half; ++c) acc[c] += acc[c + half];
       t[rt] = acc[0] * c2;
     }
-    if (more) {
+    if constexpr (MORE) {
       turn_window(kb + TURN);
       fetch_k(kb + TURN);
+      asm volatile("" ::: "memory");       // on their way before the softmax
     }
     const bool masked = kb + BK - 1 > all_see || kb + BK > k1;
 #pragma unroll
@@ -149,8 +153,13 @@ __global__ __launch_bounds__(64 * NW, RT == 4 ? 1 : 2) void chunk_rows_f32_kerne
       for (int x = 0; x < DX; ++x)
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) o[rt][x] = __builtin_amdgcn_mfma_f32_16x16x4f32(vv[i][x / 4][x % 4], t[rt][i], o[rt][x], 0, 0, 0);
-    if (more) fetch_v(kb + TURN);
-  }
+    if constexpr (MORE) {
+      fetch_v(kb + TURN);
+      asm volatile("" ::: "memory");       // and these before the next products
+    }
+  };
+  for (; kb + TURN < k1; kb += TURN) step(std::true_type{});
+  if (kb < k1) step(std::false_type{});
 
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
@@ -249,6 +258,7 @@ __global__ __launch_bounds__(256, 2) void chunk_block_f32_kernel(ChunkArgs a) {
   if (k0 < k1) {
     fetch_pages(k0);
     fetch(k0);
+    row_arrived(qv);
     place(0);
     if (k0 + BK < k1) fetch_pages(k0 + BK);
   }

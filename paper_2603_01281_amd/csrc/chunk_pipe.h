@@ -7,21 +7,21 @@
 
 namespace seka {
 
-template <int D, int HPW, int RBW>
-__global__ __launch_bounds__(64 * HPW * RBW) __attribute__((amdgpu_waves_per_eu(2, D == 64 ? 2 : 8))) void chunk_pipe_kernel(ChunkArgs pg) {
+template <int D>
+__global__ __launch_bounds__(64 * kPipeWaves) __attribute__((amdgpu_waves_per_eu(2, D == 64 ? 2 : 8))) void chunk_pipe_kernel(ChunkArgs pg) {
   AttnArgs a = {};
   a.Q = pg.Q; a.K = pg.c.K; a.V = pg.c.V; a.O = pg.O; a.lse = pg.lse;
   a.Hq = pg.Hq; a.Hkv = pg.Hkv; a.D = D; a.scale = pg.scale;
-  attention_bf16_pipe_body<D, HPW, RBW, false, 1>(a, SteerArgs{}, pg);
+  attention_bf16_pipe_body<D, 1, kPipeWaves, false, 1>(a, SteerArgs{}, pg);
 }
 
-// blockIdx: x: workgroup w whose piece starts inside a block, y: head chunk and some of its rows, four columns to a thread.  The block's
+// blockIdx: x: workgroup w whose piece starts inside a block, y: KV head and some of its rows, four columns to a thread.  The block's
 // states: the end of the piece before w, then the starts of w's and of every later piece that starts in it too.
 constexpr int kJoinThreads = 256;
-template <int D, int HPW, int RBW>
+template <int D>
 __global__ __launch_bounds__(kJoinThreads) void chunk_pipe_join_kernel(ChunkArgs pg) {
-  constexpr int BQ = 32 * RBW, ROWS = kJoinThreads / (D / 4), PARTS = HPW * BQ / ROWS;
-  const int w = blockIdx.x + 1, hc = blockIdx.y / PARTS, part = blockIdx.y % PARTS, nHC = pg.Hq / HPW;
+  constexpr int ROWS = kJoinThreads / (D / 4), PARTS = kPipeRows / ROWS;
+  const int w = blockIdx.x + 1, h = blockIdx.y / PARTS, part = blockIdx.y % PARTS, G = pg.Hq / pg.Hkv;
   const int4 here = pg.cuts[w], prev = pg.cuts[w - 1];
   if (here.z == 0 || here.x >= pg.r.B) return;
   if (prev.x == here.x && prev.y == here.y && prev.z > 0) return;      // an earlier workgroup's
@@ -35,12 +35,13 @@ __global__ __launch_bounds__(kJoinThreads) void chunk_pipe_join_kernel(ChunkArgs
     if (other) break;
   }
   const ChunkExtent e = chunk_extent(pg.r, pg.c, here.x);
-  const int r = part * ROWS + threadIdx.x / (D / 4), d = threadIdx.x % (D / 4) * 4;      // row of the workgroup: head, position
-  const int ctx = e.len - e.n, hq = hc * HPW + r / BQ;
-  const int pos = PipePlan<BQ>::first_row(e) + here.y * BQ + r % BQ, i = pos - ctx;
+  const int r = part * ROWS + threadIdx.x / (D / 4), d = threadIdx.x % (D / 4) * 4;      // row of the workgroup
+  const int ctx = e.len - e.n, base = PipePlan::first_row(e);
+  const unsigned row = (unsigned)((max(ctx, 0) - base) * G) / 32u * 32u + here.y * kPipeRows + r, at = row / (unsigned)G;      // (PipePlan::first_wave)
+  const int hq = h * G + (int)(row - at * G), pos = base + (int)at, i = pos - ctx;
   if (pos < max(ctx, 0) || i >= e.n) return;
-  const size_t stride = (size_t)2 * nHC * (HPW * BQ) * (D + 4);        // from a slot of one workgroup to the next one's
-  const float* first = pg.part + ((size_t)(2 * w) * nHC + hc) * (HPW * BQ) * (D + 4) + (size_t)r * (D + 4);       // slot 2 w; the end before it: 2 w - 1
+  const size_t stride = (size_t)2 * pg.Hkv * kPipeRows * (D + 4);      // from a slot of one workgroup to the next one's
+  const float* first = pg.part + ((size_t)(2 * w) * pg.Hkv + h) * kPipeRows * (D + 4) + (size_t)r * (D + 4);       // slot 2 w; the end before it: 2 w - 1
   const float* before = first - stride / 2;
   float m = before[D];
 #pragma unroll 4
@@ -64,31 +65,22 @@ __global__ __launch_bounds__(kJoinThreads) void chunk_pipe_join_kernel(ChunkArgs
 }
 
 struct PipeChunkPlan {
-  int hpw, rbw;          // heads and blocks of 32 rows of a workgroup
-  int width;             // workgroups per head chunk
+  int width;             // workgroups per KV head
   size_t smem, cuts, workspace;          // cuts: their offset in the workspace
 };
 
 hipError_t launch_chunk_pipe_d128(const ChunkArgs& a, const PipeChunkPlan& p, hipStream_t s);
 hipError_t launch_chunk_pipe_d64(const ChunkArgs& a, const PipeChunkPlan& p, hipStream_t s);
 
-template <int D, int HPW, int RBW>
-hipError_t launch_chunk_pipe_cfg(const ChunkArgs& a, const PipeChunkPlan& p, hipStream_t s) {
-  auto kernel = chunk_pipe_kernel<D, HPW, RBW>;
-  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)p.smem);
-  if (e != hipSuccess) return e;
-  const int nHC = a.Hq / HPW;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)(p.width * nHC)), dim3(64 * HPW * RBW), p.smem, s, a);
-  if (p.width > 1) hipLaunchKernelGGL((chunk_pipe_join_kernel<D, HPW, RBW>), dim3(p.width - 1, a.Hq * (32 * RBW) / (kJoinThreads / (D / 4))), dim3(kJoinThreads), 0, s, a);
-  return hipGetLastError();
-}
-
 template <int D>
 hipError_t launch_chunk_pipe(const ChunkArgs& a, const PipeChunkPlan& p, hipStream_t s) {
-  if (p.hpw == 4) return launch_chunk_pipe_cfg<D, 4, 2>(a, p, s);
-  if (p.hpw == 7) return launch_chunk_pipe_cfg<D, 7, 1>(a, p, s);
-  if (p.hpw == 2) return launch_chunk_pipe_cfg<D, 2, 4>(a, p, s);
-  return launch_chunk_pipe_cfg<D, 1, 8>(a, p, s);
+  auto kernel = chunk_pipe_kernel<D>;
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)p.smem);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(p.width * a.Hkv)), dim3(64 * kPipeWaves), p.smem, s, a);
+  if (p.width > 1)
+    hipLaunchKernelGGL((chunk_pipe_join_kernel<D>), dim3(p.width - 1, a.Hkv * kPipeRows / (kJoinThreads / (D / 4))), dim3(kJoinThreads), 0, s, a);
+  return hipGetLastError();
 }
 
 }  // namespace seka

@@ -1,8 +1,11 @@
 // How the blocks of query rows of a batch over a cache of pages are dealt to workgroups (attention_chunk_pipe_kernel).
 //
-// A request's new tokens are its last n of len cached ones.  Its rows are cut into blocks of BQ at positions that are multiples of
-// 32, so that a wave's 32 rows end at half a key tile; the block that starts at base + k BQ sees the keys up to its last row, which
-// is base / 32 + (k + 1) BQ / 32 half tiles.  A block costs those and kOver half tiles besides (its start and its output).
+// A request's new tokens are its last n of len cached ones.  Row (p - base) G + g is that of position p and head g of a KV head's group of G,
+// with base the multiple of 32 at or before its first new token: 32 positions are G waves of 32 rows, and no wave's rows lie on both sides of
+// the end of half a key tile, whatever G.  The waves that have new tokens, eight to a block, make up the request's blocks.  (Heads to waves of
+// their own, so that a block is 8 / G x 32 positions, left blocks of 256 positions of one head to a group of three.)
+// Block k sees the keys up to its last row, base / 32 + (w0 + 8 k + 8) / G half tiles, with w0 the first wave that has new tokens.  A block costs
+// those and kOver half tiles besides (its start and its output); all costs are in units of a G-th of half a tile.
 //
 // The blocks of all requests in a row are one axis of work of length T, which W workgroups per head chunk cut into equal pieces: a
 // piece starts and ends anywhere in a block, at a tile, and the states of a block that was cut are joined by a second kernel.  A
@@ -24,18 +27,18 @@ struct PipeCut {
   int b, k, t;           // request, block, tile
 };
 
-template <int BQ>
+constexpr int kPipeWaves = 8, kPipeRows = 32 * kPipeWaves;      // of a workgroup
+
 struct PipePlan {
-  static constexpr long long s = BQ / 32;
   ChunkRows r;
   PagedCache c;
   ChunkExtent mine;      // request `lane`, where there are no more than 64
   long long ends;        // and the half tiles of the requests up to it
-  long long T, per;      // half tiles of all blocks; of a workgroup
-  int W;                 // workgroups that get work
+  long long T, per;      // cost of all blocks; of a workgroup
+  int G, W;                // workgroups that get work
   int rem, rounds;       // a single long request: blocks that are cut, whole blocks per workgroup; rounds = 0: everything is cut
 
-  __device__ __forceinline__ PipePlan(const ChunkRows& rows, const PagedCache& cache, int width) : r(rows), c(cache), mine{0, 0, 0}, ends(0) {
+  __device__ __forceinline__ PipePlan(const ChunkRows& rows, const PagedCache& cache, int width, int group) : r(rows), c(cache), mine{0, 0, 0}, ends(0), G(group) {
     T = 0;
     const int lane = threadIdx.x & 63;
     for (int b0 = 0; b0 < r.B; b0 += 64) {
@@ -45,14 +48,14 @@ struct PipePlan {
       ends = sums(work(e));
       T += uniform(__shfl(ends, 63));
     }
-    const long long fill = T >> kPipeLeastLog2;
+    const long long fill = T < 0x80000000ll ? ((uint32_t)T >> kPipeLeastLog2) / (uint32_t)G : (T >> kPipeLeastLog2) / G;
     W = (int)(fill < 1 ? 1 : fill < width ? fill : width);
     per = T < 0x80000000ll ? (long long)(((uint32_t)T + (uint32_t)W - 1) / (uint32_t)W) : (T + W - 1) / W;
     rem = rounds = 0;
     if (r.B == 1) {
       const ChunkExtent e = extent(0);
       const int nb = blocks(e);
-      if (nb >= W && (long long)first_row(e) >= (long long)nb * BQ) {
+      if (nb >= W && first_row(e) >= e.n) {
         rounds = nb / W;
         rem = nb - rounds * W;
       }
@@ -89,13 +92,21 @@ struct PipePlan {
   }
   // position of the first block's first row
   __device__ __forceinline__ static int first_row(const ChunkExtent& e) { return max(e.len - e.n, 0) & ~31; }
-  __device__ __forceinline__ static int blocks(const ChunkExtent& e) { return e.n > 0 && e.len > 0 ? (e.len - first_row(e) + BQ - 1) / BQ : 0; }
-  __device__ __forceinline__ static int tiles(const ChunkExtent& e, int k) { return (min(e.len, first_row(e) + (k + 1) * BQ) - 1) / 64 + 1; }
-  // half tiles of the blocks 0 .. k - 1
-  __device__ __forceinline__ static long long before(const ChunkExtent& e, long long k) {
-    return k * (first_row(e) / 32 + kPipeOver) + s * (k * (k + 1) / 2);
+  // the first wave that has new tokens, of those that start at first_row
+  __device__ __forceinline__ int first_wave(const ChunkExtent& e) const { return (unsigned)((max(e.len - e.n, 0) & 31) * G) / 32u; }
+  __device__ __forceinline__ int blocks(const ChunkExtent& e) const {
+    if (e.n <= 0 || e.len <= 0) return 0;
+    const int waves = (int)((unsigned)((e.len - first_row(e)) * G + 31) / 32u) - first_wave(e);
+    return (waves + kPipeWaves - 1) / kPipeWaves;
   }
-  __device__ __forceinline__ static long long work(const ChunkExtent& e) { return before(e, blocks(e)); }
+  __device__ __forceinline__ int tiles(const ChunkExtent& e, int k) const {
+    const int rows = 32 * (first_wave(e) + kPipeWaves * (k + 1));        // behind first_row, up to the block's end
+    return (min(e.len, first_row(e) + (int)((unsigned)(rows - 1) / (unsigned)G) + 1) - 1) / 64 + 1;
+  }
+  // cost of the blocks 0 .. k - 1
+  __device__ __forceinline__ long long of_each(const ChunkExtent& e) const { return (long long)(first_row(e) / 32 + kPipeOver) * G + first_wave(e); }
+  __device__ __forceinline__ long long before(const ChunkExtent& e, long long k) const { return k * of_each(e) + kPipeWaves * (k * (k + 1) / 2); }
+  __device__ __forceinline__ long long work(const ChunkExtent& e) const { return before(e, blocks(e)); }
 
   // block k's index of round i for workgroup w: back and forth
   __device__ __forceinline__ int whole(int w, int i) const { return rem + i * W + (i & 1 ? W - 1 - w : w); }
@@ -139,18 +150,19 @@ struct PipePlan {
     return PipeCut{r.B, 0, 0};
   }
 
-  // The place x half tiles into the first nb blocks of a request.
-  __device__ __forceinline__ static PipeCut at(const ChunkExtent& e, int b, int nb, long long x) {
+  // The place x into the first nb blocks of a request.
+  __device__ __forceinline__ PipeCut at(const ChunkExtent& e, int b, int nb, long long x) const {
+    constexpr float s = kPipeWaves;
     // the last block that starts at x or before: s k (k + 1) / 2 + k f = x, put right by whole blocks (fp32: off by a few of millions)
-    const float f = (float)(first_row(e) / 32 + kPipeOver) + 0.5f * s;
+    const float f = (float)of_each(e) + 0.5f * s;
     const float root = 2.f * (float)x / (f + sqrtf(f * f + 2.f * s * (float)x));
     int k = min(max((int)root, 0), nb);
     while (k > 0 && before(e, k) > x) --k;
     while (k < nb && before(e, k + 1) <= x) ++k;
     k = uniform(k);
     if (k >= nb) return PipeCut{b, nb, 0};
-    const long long into = x - before(e, k) - kPipeOver;
-    const int n = tiles(e, k), t = uniform((int)(into < 0 ? 0 : into / 2));
+    const long long into = x - before(e, k) - (long long)kPipeOver * G;      // less than of_each and kPipeWaves k
+    const int n = tiles(e, k), t = uniform((int)(into < 0 ? 0u : (uint32_t)into / (uint32_t)(2 * G)));
     if (t < kPipeSnap) return PipeCut{b, k, 0};
     if (n - t < kPipeSnap) return PipeCut{b, k + 1, 0};
     return PipeCut{b, k, t};
@@ -165,14 +177,13 @@ struct PipePiece {
 };
 
 // The pieces of workgroup w in turn.
-template <int BQ>
 struct PipePieces {
-  PipePlan<BQ> p;
+  PipePlan p;
   int w, round;
   PipeCut now, end, start;
 
-  __device__ __forceinline__ PipePieces(const ChunkRows& rows, const PagedCache& cache, int width, int workgroup)
-      : p(rows, cache, width), w(workgroup), round(0) {
+  __device__ __forceinline__ PipePieces(const ChunkRows& rows, const PagedCache& cache, int width, int group, int workgroup)
+      : p(rows, cache, width, group), w(workgroup), round(0) {
     now = end = start = PipeCut{p.r.B, 0, 0};
     if (w >= p.W) {
       round = p.rounds;
@@ -184,11 +195,11 @@ struct PipePieces {
   __device__ __forceinline__ bool next(PipePiece& out) {
     while (now.b < p.r.B && (now.b < end.b || (now.b == end.b && (now.k < end.k || (now.k == end.k && now.t < end.t))))) {
       const ChunkExtent e = p.extent(now.b);
-      if (now.k >= PipePlan<BQ>::blocks(e)) {
+      if (now.k >= p.blocks(e)) {
         now = PipeCut{now.b + 1, 0, 0};
         continue;
       }
-      const int n = PipePlan<BQ>::tiles(e, now.k);
+      const int n = p.tiles(e, now.k);
       const bool last = now.b == end.b && now.k == end.k;
       out = PipePiece{now.b, now.k, now.t, last ? end.t : n, n, e, false};
       out.whole = out.t0 == 0 && out.t1 == n;
@@ -197,7 +208,7 @@ struct PipePieces {
     }
     if (round < p.rounds) {
       const ChunkExtent e = p.extent(0);
-      const int k = p.whole(w, round), n = PipePlan<BQ>::tiles(e, k);
+      const int k = p.whole(w, round), n = p.tiles(e, k);
       ++round;
       out = PipePiece{0, k, 0, n, n, e, true};
       return true;

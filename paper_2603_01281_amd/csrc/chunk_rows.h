@@ -57,6 +57,15 @@ __device__ __forceinline__ void merge_waves(const ChunkArgs& a, const ChunkItem&
   }
 }
 
+// Queries have arrived here: their registers are not waited for in the loop, which would wait for the loads of the next keys with them.
+template <typename V, int A, int B>
+__device__ __forceinline__ void row_arrived(V (&q)[A][B]) {
+#pragma unroll
+  for (int a = 0; a < A; ++a)
+#pragma unroll
+    for (int b = 0; b < B; ++b) asm volatile("" : "+v"(q[a][b]));
+}
+
 // What the joining kernel has to know of an item: how many ranges its chunk has (0: not the chunk's first, or no item), where its rows are.
 __device__ __forceinline__ void row_describe(const ChunkArgs& a, bool exists, const ChunkItem& it) {
   if (blockIdx.y == 0 && threadIdx.x == 0)
