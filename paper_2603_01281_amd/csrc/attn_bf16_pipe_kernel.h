@@ -207,28 +207,6 @@ constexpr int pipe_element_at(int m, int mfmas) {
 
 struct PipeDense {};             // the arguments of pages where there are none
 
-// New tokens that see no key (more of them than cached tokens): the requests item, item + width, .. of a KV head.
-template <int D>
-__device__ __forceinline__ void pipe_rows_without_keys(const ChunkArgs& pg, int item, int h) {
-  const int lane = threadIdx.x & 63, G = pg.Hq / pg.Hkv;
-  for (int b0 = 0; b0 < pg.r.B; b0 += 64) {
-    ChunkExtent e = {0, 0, 0};
-    const int mine = b0 + lane;
-    if (mine < pg.r.B && mine % pg.width == item) e = chunk_extent(pg.r, pg.c, mine);
-    unsigned long long todo = __ballot(e.n > e.len);
-    for (; todo; todo &= todo - 1) {       // rare: lengths that do not count the new tokens
-      const int l = __builtin_ctzll(todo);
-      const int rows = __shfl(e.n - e.len, l), row0 = __shfl(e.row0, l);
-      for (int x = threadIdx.x; x < rows * G * (D / 8); x += blockDim.x) {
-        const size_t row = (size_t)(row0 + x / (G * (D / 8))) * pg.Hq + h * G;
-        reinterpret_cast<uint4*>(static_cast<uint16_t*>(pg.O) + row * D)[x % (G * (D / 8))] = make_uint4(0, 0, 0, 0);
-      }
-      if (pg.lse)
-        for (int x = threadIdx.x; x < rows * G; x += blockDim.x) pg.lse[(size_t)(h * G + x % G) * pg.r.total + row0 + x / G] = -INFINITY;
-    }
-  }
-}
-
 template <class PIECES, class PG>
 __device__ __forceinline__ PIECES pipe_pieces_of(const PG& pg, int item) {
   if constexpr (std::is_same_v<PG, PipeDense>) return PIECES{};
@@ -244,7 +222,7 @@ template <int D, int HPW, int RBW, bool STEER, int NKR, class PG>
 __device__ __forceinline__ void attention_bf16_pipe_body(const AttnArgs& a, const SteerArgs& st, const PG& pg) {
   constexpr bool PAGED = !std::is_same_v<PG, PipeDense>;
   static_assert(!(PAGED && STEER), "keys in pages are edited before they are stored");
-  static_assert(!PAGED || (HPW == 1 && RBW == kPipeWaves), "rows of the plan");
+  static_assert(!PAGED || (HPW == 1 && RBW == PipeBf16::WAVES), "rows of the plan");
   static_assert(D == 64 || D == 128, "head dimensions of the tile layouts");
   constexpr int NW = HPW * RBW;
   constexpr int NT = 64 * NW;
@@ -297,7 +275,7 @@ __device__ __forceinline__ void attention_bf16_pipe_body(const AttnArgs& a, cons
   size_t tok0;                               // first token of this prompt in the tensors
   int S;                                     // this prompt's length: rows and keys beyond it do not exist
   int nblocks, qb;
-  using Pieces = std::conditional_t<PAGED, PipePieces, PipeDense>;
+  using Pieces = std::conditional_t<PAGED, PipePieces<PipeBf16>, PipeDense>;
   [[maybe_unused]] Pieces pieces = pipe_pieces_of<Pieces>(pg, item);
   [[maybe_unused]] PipePiece piece = {};
   [[maybe_unused]] int key0 = 0;             // the piece's first key
@@ -309,8 +287,8 @@ __device__ __forceinline__ void attention_bf16_pipe_body(const AttnArgs& a, cons
       key0 = 64 * piece.t0;
       S = piece.e.len - key0;
       const int ctx = piece.e.len - piece.e.n;
-      first_row = PipePlan::first_row(piece.e) - key0;
-      first_wave = pieces.p.first_wave(piece.e) + kPipeWaves * piece.k;
+      first_row = pipe_first_row(piece.e) - key0;
+      first_wave = pipe_first_wave(piece.e, G) + NW * piece.k;
       first_new = max(ctx, 0) - key0;
       tok0 = (size_t)((long long)piece.e.row0 - ctx + key0);       // row of the tensors of position 0
       b = piece.b;
@@ -319,7 +297,7 @@ __device__ __forceinline__ void attention_bf16_pipe_body(const AttnArgs& a, cons
   if constexpr (PAGED) {
     slot = nblocks = qb = 0;
     if (hc == 0 && threadIdx.x == 0) pg.cuts[item] = make_int4(pieces.start.b, pieces.start.k, pieces.start.t, 0);
-    pipe_rows_without_keys<D>(pg, item, hc);
+    pipe_rows_without_keys<uint16_t, D>(pg, item, hc);
     if (!pieces.next(piece)) return;         // workgroup-uniform, before any barrier
     take_piece();
   } else {

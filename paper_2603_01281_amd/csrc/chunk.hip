@@ -221,8 +221,6 @@ hipError_t launch_rows(const ChunkArgs& a, const RowPlan& r, hipStream_t s) {
   return hipGetLastError();
 }
 
-constexpr double kBlockLeastFlops = 1e9;
-
 // Rows per workgroup, ranges and the bounds of both, from what the host knows: B requests, `total` new tokens of which no request
 // has more than max_q, caches of up to S tokens.
 RowPlan row_plan(int B, int S, int Hq, int Hkv, int D, int dtype, int total, int max_q) {
@@ -234,17 +232,15 @@ RowPlan row_plan(int B, int S, int Hq, int Hkv, int D, int dtype, int total, int
   r.p.least = bf16 ? 8 : 4;                // 256 tokens, 128: a block of every wave of eight
   const long long ranges = std::max(1, std::min(kMaxRanges, (blocks + r.p.least - 1) / r.p.least));
   auto chunks_of = [&](int R) { return std::min(((long long)total * G) / R + B, 0x3fffffffll); };
-  // fp32 chunks that are long enough, and enough of them, for waves with rows of their own that share their keys
-  r.block = !bf16 && rows > 64 && 4.0 * D * total * Hq * S > kBlockLeastFlops;
   // as many tiles of 16 rows as there are, up to two (D = 64: four), but no more than leave two workgroups for every compute unit.  Four at
   // D = 128 need the registers of two waves: 10 new tokens over 24967, 32 / 8 heads, 60.1 us, in two chunks of two tiles 32.5.
   r.rows16 = rows <= 16 ? 1 : rows <= 32 || D == 128 ? 2 : 4;
-  while (!r.block && r.rows16 > 1 && chunks_of(16 * r.rows16) * ranges * Hkv < 512) r.rows16 /= 2;
-  r.p.R = r.block ? kBlockRows : 16 * r.rows16;
+  while (r.rows16 > 1 && chunks_of(16 * r.rows16) * ranges * Hkv < 512) r.rows16 /= 2;
+  r.p.R = 16 * r.rows16;
   r.rows = (int)std::min(rows, (long long)r.p.R);
   const long long chunks = chunks_of(r.p.R);
   // eight waves to a workgroup where the keys are few: a range is then half as long a chain
-  const bool few = !r.block && r.rows16 <= 2 && chunks * blocks * Hkv <= 256 * 8 * 2 && chunks * Hkv <= 256;
+  const bool few = r.rows16 <= 2 && chunks * blocks * Hkv <= 256 * 8 * 2 && chunks * Hkv <= 256;
   r.waves = few ? 8 : 4;
   // two workgroups of four waves to a compute unit, about, or one of eight
   r.p.slots_log2 = 0;
@@ -274,15 +270,18 @@ int compute_units() {
 // n=1000 S=1000 52.4 / 37.9; 3.4e10 n=512 S=4096 103 / 53.5.
 constexpr double kPipeLeastFlops = 3.5e9;
 
-// Whether a call's chunks go to the pipelined kernel, and how: bf16, more rows per KV head than four tiles of 16, and a cache
-// whose page numbers fit beside the tiles in LDS (4 bytes for every page of S tokens).
+constexpr double kBlockLeastFlops = 1e9;
+
+// Whether a call's chunks go to a kernel whose waves have rows of their own, and how: more rows per KV head than four tiles of 16, and, bf16, a
+// cache whose page numbers fit beside the tiles in LDS (4 bytes for every page of S tokens).
 bool pipe_plan(int S, int Hq, int Hkv, int D, int dtype, int shift, int total, int max_q, PipeChunkPlan* out) {
   const int G = Hq / Hkv;
-  if (dtype != SEKA_BF16 || (long long)std::min(max_q, total) * G <= 64) return false;
-  if (4.0 * D * total * Hq * S <= kPipeLeastFlops) return false;
-  out->width = std::max(1, compute_units() / Hkv);
-  out->smem = attention_bf16_pipe_smem_bytes(D, 0, false, 1, kPipeWaves) + (((size_t)S >> shift) + 2) * sizeof(int);
-  out->cuts = (size_t)2 * out->width * Hkv * kPipeRows * (D + 4) * sizeof(float);      // behind the states, two per workgroup
+  const bool bf16 = dtype == SEKA_BF16;
+  if ((long long)std::min(max_q, total) * G <= 64) return false;
+  if (4.0 * D * total * Hq * S <= (bf16 ? kPipeLeastFlops : kBlockLeastFlops)) return false;
+  out->width = std::max(1, (bf16 ? 1 : 2) * compute_units() / Hkv);      // workgroups to a compute unit
+  out->smem = !bf16 ? 0 : attention_bf16_pipe_smem_bytes(D, 0, false, 1, PipeBf16::WAVES) + (((size_t)S >> shift) + 2) * sizeof(int);
+  out->cuts = (size_t)2 * out->width * Hkv * (bf16 ? PipeBf16::ROWS : PipeF32::ROWS) * (D + 4) * sizeof(float);      // behind the states, two per workgroup
   out->workspace = out->cuts + (size_t)out->width * sizeof(int4);
   return out->smem <= 160 * 1024;
 }
@@ -308,6 +307,7 @@ hipError_t launch_chunk(ChunkArgs a, int D, int dtype, int S, hipStream_t s) {
   if (pipe_plan(S, a.Hq, a.Hkv, D, dtype, a.c.shift, a.r.total, a.r.max_q, &p)) {
     a.width = p.width;
     a.cuts = reinterpret_cast<int4*>(reinterpret_cast<char*>(a.part) + p.cuts);
+    if (dtype == SEKA_F32) return launch_chunk_block_f32(a, D, p, s);
     return D == 128 ? launch_chunk_pipe_d128(a, p, s) : launch_chunk_pipe_d64(a, p, s);
   }
   const RowPlan r = row_plan(a.r.B, S, a.Hq, a.Hkv, D, dtype, a.r.total, a.r.max_q);

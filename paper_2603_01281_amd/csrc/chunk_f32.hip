@@ -6,6 +6,7 @@
 // K and V go from the pages straight into operand registers with 16-byte loads, those of the wave's next 16 keys as soon as its
 // products with these are issued.  A score is shared by several accumulators: short chains of sums, and no product waits for
 // the one before it.
+#include "chunk_join.h"
 #include "chunk_rows.h"
 
 namespace seka {
@@ -181,165 +182,214 @@ __global__ __launch_bounds__(64 * NW, RT == 4 ? 1 : 2) void chunk_rows_f32_kerne
   }
 }
 
-// Long chunks: waves of 32 rows each that share the keys.  Tiles of 32 keys and values pass through LDS, double-buffered, loaded to
+// Long chunks (chunk_plan.h): waves of 32 rows each that share the keys.  Tiles of 32 keys and values pass through LDS, double-buffered, loaded to
 // registers a tile ahead and their page numbers two; a tile's operands are read from LDS once per 32 rows.  Matrix instructions bound it: 256
-// of 32 cycles per tile and wave (D = 128) beside 32 LDS reads.
+// of 32 cycles per tile and wave (D = 128) beside 32 LDS reads.  Where no more than two waves have rows, two waves each take them and half of a tile.
 template <int D>
 __global__ __launch_bounds__(256, 2) void chunk_block_f32_kernel(ChunkArgs a) {
-  constexpr int RT = 2, NW = 4, BK = 32, KI = D / 16, VH = D / 64, DX = D / 16, LD = D + 4;
+  constexpr int RT = 2, NW = PipeF32::WAVES, BK = 32, KI = D / 16, VH = D / 64, DX = D / 16, LD = D + 4;
   constexpr int CPR = D / 4, NL = BK * CPR / 256, RPP = 256 / CPR;       // 16-byte pieces per row, loads per thread, rows per pass
-  static_assert(NW * 16 * RT == kBlockRows, "rows of the plan");
-  __shared__ __attribute__((aligned(16))) float kt_lds[2][BK * LD], vt_lds[2][BK * LD];
+  __shared__ __attribute__((aligned(16))) float tiles[4][BK * LD];
+  float (*const kt_lds)[BK * LD] = tiles, (*const vt_lds)[BK * LD] = tiles + 2;
+  static_assert(NW == 4 && 2 * RT * (DX + 1) * 64 * 4 <= 4 * BK * LD, "states of two waves in the tiles");
 
-  ChunkItem it;
-  const bool exists = plan_item(a.r, a.c, a.p, blockIdx.x, it);
-  row_describe(a, exists, it);
-  if (!exists) return;                     // workgroup-uniform
-  int k0, k1;
-  plan_range(a.p, it, k0, k1);
-  const int h = blockIdx.y, G = a.p.G, tid = threadIdx.x;
+  const int h = blockIdx.x % a.Hkv, item = blockIdx.x / a.Hkv, G = a.Hq / a.Hkv, tid = threadIdx.x;
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, g = lane >> 4;
-  const int nrows = it.e.n * G, ctx = it.e.len - it.e.n, row_first = it.rc * kBlockRows + 32 * wave;
-
-  f32x4 qv[RT][KI];                        // d = 16 x + 4 g + e
-  int last[RT];
-#pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    const int row = row_first + 16 * rt + l16;
-    const bool ok = row < nrows;
-    const int i = ok ? row / G : 0, hd = ok ? row - i * G : 0;
-    last[rt] = ok ? ctx + i : -1;
-    const float* qp = static_cast<const float*>(a.Q) + ((size_t)(it.e.row0 + i) * a.Hq + h * G + hd) * D + 4 * g;
-#pragma unroll
-    for (int x = 0; x < KI; ++x) {
-      qv[rt][x] = f32x4{0.f, 0.f, 0.f, 0.f};
-      if (ok) qv[rt][x] = *reinterpret_cast<const f32x4*>(qp + 16 * x);
-    }
-  }
-  const int all_see = ctx + row_first / G;                                       // keys up to here are seen by all of the wave's rows,
-  const int some_see = row_first < nrows ? ctx + (min(row_first + 32, nrows) - 1) / G : -1;      // behind here by none
+  PipePieces<PipeF32> pieces(a.r, a.c, a.width, G, item);
+  if (h == 0 && tid == 0) a.cuts[item] = make_int4(pieces.start.b, pieces.start.k, pieces.start.t, 0);
+  pipe_rows_without_keys<float, D>(a, item, h);
 
   const size_t row_floats = (size_t)a.Hkv * D;
-  const int slots = (1 << a.c.shift) - 1, row = tid / CPR, piece = 4 * (tid % CPR);
-  const float* Kh = static_cast<const float*>(a.c.K) + (size_t)h * D + piece;
-  const float* Vh = static_cast<const float*>(a.c.V) + (size_t)h * D + piece;
-  int pages[NL];
-  f32x4 kn[NL], vn[NL];
-  auto fetch_pages = [&](int kb) __attribute__((always_inline)) {
-#pragma unroll
-    for (int x = 0; x < NL; ++x) pages[x] = page_of(a.c, it.b, min(kb + row + RPP * x, k1 - 1));
-  };
-  auto fetch = [&](int kb) __attribute__((always_inline)) {                      // rows behind the last key repeat it
-#pragma unroll
-    for (int x = 0; x < NL; ++x) {
-      const size_t off = (((size_t)pages[x] << a.c.shift) + (min(kb + row + RPP * x, k1 - 1) & slots)) * row_floats;
-      kn[x] = *reinterpret_cast<const f32x4*>(Kh + off);
-      vn[x] = *reinterpret_cast<const f32x4*>(Vh + off);
-    }
-  };
-  auto place = [&](int buf) __attribute__((always_inline)) {
-#pragma unroll
-    for (int x = 0; x < NL; ++x) {
-      *reinterpret_cast<f32x4*>(&kt_lds[buf][(row + RPP * x) * LD + piece]) = kn[x];
-      *reinterpret_cast<f32x4*>(&vt_lds[buf][(row + RPP * x) * LD + piece]) = vn[x];
-    }
-  };
-
-  f32x4 o[RT][DX];
-  float m[RT], l[RT];
-#pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    m[rt] = kRowLow;
-    l[rt] = 0.f;
-#pragma unroll
-    for (int x = 0; x < DX; ++x) o[rt][x] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
+  const int slots = (1 << a.c.shift) - 1, row = tid / CPR, part = 4 * (tid % CPR);
+  const float* Kh = static_cast<const float*>(a.c.K) + (size_t)h * D + part;
+  const float* Vh = static_cast<const float*>(a.c.V) + (size_t)h * D + part;
   const float c2 = a.scale * 1.4426950408889634f;
-  if (k0 < k1) {
+  PipePiece piece;
+  while (pieces.next(piece)) {             // workgroup-uniform
+    const ChunkExtent e = piece.e;
+    const int ctx = e.len - e.n, first = max(ctx, 0), base = pipe_first_row(e), wave0 = pipe_first_wave(e, G) + NW * piece.k;
+    const bool halves = pieces.p.half(e, piece.k);
+    const int rows_of = halves ? wave & 1 : wave;                        // the wave of the block whose rows these are
+    const unsigned row_first = 32u * (unsigned)(wave0 + rows_of);
+    f32x4 qv[RT][KI];                      // d = 16 x + 4 g + e
+    int last[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      const unsigned r = row_first + 16 * rt + l16, at = r / (unsigned)G;
+      const int pos = base + (int)at;
+      const bool ok = pos >= first && pos < e.len;
+      last[rt] = ok ? pos : -1;
+      const float* qp = static_cast<const float*>(a.Q) + ((size_t)(e.row0 + (ok ? pos - ctx : 0)) * a.Hq + h * G + (ok ? (int)(r - at * G) : 0)) * D + 4 * g;
+#pragma unroll
+      for (int x = 0; x < KI; ++x) {
+        qv[rt][x] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (ok) qv[rt][x] = *reinterpret_cast<const f32x4*>(qp + 16 * x);
+      }
+    }
+    const int pos0 = base + (int)(row_first / (unsigned)G);
+    const int all_see = max(pos0, first);                                          // keys up to here are seen by all of the wave's rows,
+    const int some_see = pos0 < e.len ? min(base + (int)((row_first + 31) / (unsigned)G), e.len - 1) : -1;         // behind here by none
+    const int k0 = 64 * piece.t0;
+    const int k1 = min(64 * piece.t1, min(e.len, base + (int)((32u * (unsigned)(wave0 + NW) - 1) / (unsigned)G) + 1));
+
+    int pages[NL];
+    f32x4 kn[NL], vn[NL];
+    auto fetch_pages = [&](int kb) __attribute__((always_inline)) {
+#pragma unroll
+      for (int x = 0; x < NL; ++x) pages[x] = page_of(a.c, piece.b, min(kb + row + RPP * x, k1 - 1));
+    };
+    auto fetch = [&](int kb) __attribute__((always_inline)) {                      // rows behind the last key repeat it
+#pragma unroll
+      for (int x = 0; x < NL; ++x) {
+        const size_t off = (((size_t)pages[x] << a.c.shift) + (min(kb + row + RPP * x, k1 - 1) & slots)) * row_floats;
+        kn[x] = *reinterpret_cast<const f32x4*>(Kh + off);
+        vn[x] = *reinterpret_cast<const f32x4*>(Vh + off);
+      }
+    };
+    auto place = [&](int buf) __attribute__((always_inline)) {
+#pragma unroll
+      for (int x = 0; x < NL; ++x) {
+        *reinterpret_cast<f32x4*>(&kt_lds[buf][(row + RPP * x) * LD + part]) = kn[x];
+        *reinterpret_cast<f32x4*>(&vt_lds[buf][(row + RPP * x) * LD + part]) = vn[x];
+      }
+    };
+
+    f32x4 o[RT][DX];
+    float m[RT], l[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      m[rt] = kRowLow;
+      l[rt] = 0.f;
+#pragma unroll
+      for (int x = 0; x < DX; ++x) o[rt][x] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    // 16 keys of a tile: half h16 of the one that starts at kb
+    auto half_tile = [&](int kb, int h16, int buf) __attribute__((always_inline)) {
+      const float* Kt = kt_lds[buf];
+      const float* Vt = vt_lds[buf];
+      const bool masked = kb + BK - 1 > all_see || kb + BK > k1;
+      f32x4 acc[RT][2];                    // even and odd products: two chains per tile of rows
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) acc[rt][0] = acc[rt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int x = 0; x < KI; ++x) {
+        const f32x4 kf = *reinterpret_cast<const f32x4*>(Kt + (16 * h16 + l16) * LD + 16 * x + 4 * g);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) acc[rt][e & 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[e], qv[rt][x][e], acc[rt][e & 1], 0, 0, 0);
+      }
+      f32x4 t[RT];
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        t[rt] = (acc[rt][0] + acc[rt][1]) * c2;
+        float top = kRowLow;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (masked && kb + 16 * h16 + 4 * g + i > last[rt]) t[rt][i] = -INFINITY;
+          top = fmaxf(top, t[rt][i]);
+        }
+        top = groups_max(top);
+        const bool raise = top > m[rt] + kRowSlack;
+        if (__any(raise)) {
+          const float f = raise ? __builtin_amdgcn_exp2f(m[rt] - top) : 1.f;
+          if (raise) m[rt] = top;
+          l[rt] *= f;
+#pragma unroll
+          for (int x = 0; x < DX; ++x) o[rt][x] *= f;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          t[rt][i] = __builtin_amdgcn_exp2f(t[rt][i] - m[rt]);
+          l[rt] += t[rt][i];
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int hh = 0; hh < VH; ++hh) {
+          const f32x4 vf = *reinterpret_cast<const f32x4*>(Vt + (16 * h16 + 4 * g + i) * LD + 64 * hh + 4 * l16);
+#pragma unroll
+          for (int x = 0; x < 4; ++x)
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) o[rt][4 * hh + x] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[x], t[rt][i], o[rt][4 * hh + x], 0, 0, 0);
+        }
+    };
     fetch_pages(k0);
     fetch(k0);
     row_arrived(qv);
     place(0);
     if (k0 + BK < k1) fetch_pages(k0 + BK);
-  }
-  __syncthreads();
-  int buf = 0;
-  for (int kb = k0; kb < k1; kb += BK, buf ^= 1) {
-    const bool more = kb + BK < k1;
-    if (more) {
-      fetch(kb + BK);
-      if (kb + 2 * BK < k1) fetch_pages(kb + 2 * BK);
+    __syncthreads();
+    int buf = 0;
+    for (int kb = k0; kb < k1; kb += BK, buf ^= 1) {
+      const bool more = kb + BK < k1;
+      if (more) {
+        fetch(kb + BK);
+        if (kb + 2 * BK < k1) fetch_pages(kb + 2 * BK);
+      }
+      if (kb <= some_see) {                // wave-uniform
+#pragma nounroll
+        for (int h16 = halves ? wave >> 1 : 0; h16 < (halves ? (wave >> 1) + 1 : 2); ++h16) half_tile(kb, h16, buf);
+      }
+      if (more) place(buf ^ 1);            // read by nobody since the barrier before
+      __syncthreads();
     }
-    if (kb <= some_see) {                  // wave-uniform
-      const float* Kt = kt_lds[buf];
-      const float* Vt = vt_lds[buf];
-      const bool masked = kb + BK - 1 > all_see || kb + BK > k1;
+
+    float lt[RT];
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        f32x4 acc[RT][2];                  // even and odd products: two chains per tile of rows
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) acc[rt][0] = acc[rt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int x = 0; x < KI; ++x) {
-          const f32x4 kf = *reinterpret_cast<const f32x4*>(Kt + (16 * half + l16) * LD + 16 * x + 4 * g);
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt) acc[rt][e & 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[e], qv[rt][x][e], acc[rt][e & 1], 0, 0, 0);
-        }
-        f32x4 t[RT];
+    for (int rt = 0; rt < RT; ++rt) lt[rt] = groups_sum(l[rt]);
+    if (halves) {                          // waves 2 and 3 hand theirs over, lane by lane
+      f32x4* const at = reinterpret_cast<f32x4*>(&tiles[0][0]) + rows_of * RT * (DX + 1) * 64 + lane;
+      if (wave >= 2) {
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
-          t[rt] = (acc[rt][0] + acc[rt][1]) * c2;
-          float top = kRowLow;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            if (masked && kb + 16 * half + 4 * g + i > last[rt]) t[rt][i] = -INFINITY;
-            top = fmaxf(top, t[rt][i]);
-          }
-          top = groups_max(top);
-          const bool raise = top > m[rt] + kRowSlack;
-          if (__any(raise)) {
-            const float f = raise ? __builtin_amdgcn_exp2f(m[rt] - top) : 1.f;
-            if (raise) m[rt] = top;
-            l[rt] *= f;
-#pragma unroll
-            for (int x = 0; x < DX; ++x) o[rt][x] *= f;
-          }
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            t[rt][i] = __builtin_amdgcn_exp2f(t[rt][i] - m[rt]);
-            l[rt] += t[rt][i];
-          }
+          for (int x = 0; x < DX; ++x) at[(rt * (DX + 1) + x) * 64] = o[rt][x];
+          at[(rt * (DX + 1) + DX) * 64] = f32x4{m[rt], lt[rt], 0.f, 0.f};
         }
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int hh = 0; hh < VH; ++hh) {
-            const f32x4 vf = *reinterpret_cast<const f32x4*>(Vt + (16 * half + 4 * g + i) * LD + 64 * hh + 4 * l16);
-#pragma unroll
-            for (int x = 0; x < 4; ++x)
-#pragma unroll
-              for (int rt = 0; rt < RT; ++rt) o[rt][4 * hh + x] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[x], t[rt][i], o[rt][4 * hh + x], 0, 0, 0);
-          }
       }
-    }
-    if (more) place(buf ^ 1);              // read by nobody since the barrier before
-    __syncthreads();
-  }
-
+      __syncthreads();
+      if (wave < 2) {
 #pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    const float lt = groups_sum(l[rt]);
-    const int r = row_first + 16 * rt + l16;
-    if (r < nrows) {
+        for (int rt = 0; rt < RT; ++rt) {
+          const f32x4 ml = at[(rt * (DX + 1) + DX) * 64];
+          const float mm = fmaxf(m[rt], ml[0]), f = __builtin_amdgcn_exp2f(m[rt] - mm), f2 = __builtin_amdgcn_exp2f(ml[0] - mm);
+          m[rt] = mm;
+          lt[rt] = lt[rt] * f + ml[1] * f2;
 #pragma unroll
-      for (int hh = 0; hh < VH; ++hh)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int d = 64 * hh + 16 * g + 4 * i;
-          row_emit<float, D>(a, it, h, r, d, m[rt], lt, f32x4{o[rt][4 * hh][i], o[rt][4 * hh + 1][i], o[rt][4 * hh + 2][i], o[rt][4 * hh + 3][i]});
+          for (int x = 0; x < DX; ++x) o[rt][x] = o[rt][x] * f + at[(rt * (DX + 1) + x) * 64] * f2;
         }
+      }
+      __syncthreads();                     // the tiles are free
+    }
+    if (!halves || wave < 2) {
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        if (last[rt] < 0) continue;
+        const unsigned r = row_first + 16 * rt + l16;
+        const int head = h * G + (int)(r % (unsigned)G);
+        const size_t token = (size_t)(e.row0 + last[rt] - ctx);
+        float* dst;
+        float f = 1.f;
+        if (piece.whole) {
+          dst = static_cast<float*>(a.O) + (token * a.Hq + head) * D;
+          f = 1.f / lt[rt];
+          if (a.lse && g == 0) a.lse[(size_t)head * a.r.total + token] = m[rt] * 0.6931471805599453f + logf(lt[rt]);
+        } else {
+          dst = a.part + (((size_t)pieces.slot(piece) * a.Hkv + h) * PipeF32::ROWS + 32 * rows_of + 16 * rt + l16) * (D + 4);
+          if (g == 0) {
+            dst[D] = m[rt];
+            dst[D + 1] = lt[rt];
+          }
+        }
+#pragma unroll
+        for (int hh = 0; hh < VH; ++hh)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            *reinterpret_cast<f32x4*>(dst + 64 * hh + 16 * g + 4 * i) =
+                f32x4{o[rt][4 * hh][i], o[rt][4 * hh + 1][i], o[rt][4 * hh + 2][i], o[rt][4 * hh + 3][i]} * f;
+      }
     }
   }
 }
@@ -354,14 +404,24 @@ void launch_rows(const ChunkArgs& a, const RowPlan& r, hipStream_t s) {
 
 template <int D>
 hipError_t launch_rows(const ChunkArgs& a, const RowPlan& r, hipStream_t s) {
-  if (r.block) hipLaunchKernelGGL((chunk_block_f32_kernel<D>), dim3(r.items, a.Hkv), dim3(256), 0, s, a);
-  else if (r.waves == 8) launch_rows<D, 8>(a, r, s);
+  if (r.waves == 8) launch_rows<D, 8>(a, r, s);
   else launch_rows<D, 4>(a, r, s);
   launch_chunk_merge<float, D>(a, r.items, r.rows, s);
   return hipGetLastError();
 }
 
+template <int D>
+hipError_t launch_block(const ChunkArgs& a, const PipeChunkPlan& p, hipStream_t s) {
+  hipLaunchKernelGGL((chunk_block_f32_kernel<D>), dim3((unsigned)(p.width * a.Hkv)), dim3(64 * PipeF32::WAVES), 0, s, a);
+  launch_chunk_join<float, PipeF32, D>(a, p, s);
+  return hipGetLastError();
+}
+
 }  // namespace
+
+hipError_t launch_chunk_block_f32(const ChunkArgs& a, int D, const PipeChunkPlan& p, hipStream_t s) {
+  return D == 128 ? launch_block<128>(a, p, s) : launch_block<64>(a, p, s);
+}
 
 hipError_t launch_chunk_f32(const ChunkArgs& a, int D, const RowPlan& r, hipStream_t s) {
   return D == 128 ? launch_rows<128>(a, r, s) : launch_rows<64>(a, r, s);

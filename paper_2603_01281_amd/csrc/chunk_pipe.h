@@ -1,73 +1,19 @@
-// seka_attention_chunk for long chunks, bf16: the software-pipelined prefill kernel over pages (attn_bf16_pipe_kernel.h), and the kernel that
-// joins the blocks of rows that were cut.
+// seka_attention_chunk for long chunks, bf16: the software-pipelined prefill kernel over pages (attn_bf16_pipe_kernel.h).
 #pragma once
 #include <algorithm>
 
 #include "attn_bf16_pipe_kernel.h"
+#include "chunk_join.h"
 
 namespace seka {
 
 template <int D>
-__global__ __launch_bounds__(64 * kPipeWaves) __attribute__((amdgpu_waves_per_eu(2, D == 64 ? 2 : 8))) void chunk_pipe_kernel(ChunkArgs pg) {
+__global__ __launch_bounds__(64 * PipeBf16::WAVES) __attribute__((amdgpu_waves_per_eu(2, D == 64 ? 2 : 8))) void chunk_pipe_kernel(ChunkArgs pg) {
   AttnArgs a = {};
   a.Q = pg.Q; a.K = pg.c.K; a.V = pg.c.V; a.O = pg.O; a.lse = pg.lse;
   a.Hq = pg.Hq; a.Hkv = pg.Hkv; a.D = D; a.scale = pg.scale;
-  attention_bf16_pipe_body<D, 1, kPipeWaves, false, 1>(a, SteerArgs{}, pg);
+  attention_bf16_pipe_body<D, 1, PipeBf16::WAVES, false, 1>(a, SteerArgs{}, pg);
 }
-
-// blockIdx: x: workgroup w whose piece starts inside a block, y: KV head and some of its rows, four columns to a thread.  The block's
-// states: the end of the piece before w, then the starts of w's and of every later piece that starts in it too.
-constexpr int kJoinThreads = 256;
-template <int D>
-__global__ __launch_bounds__(kJoinThreads) void chunk_pipe_join_kernel(ChunkArgs pg) {
-  constexpr int ROWS = kJoinThreads / (D / 4), PARTS = kPipeRows / ROWS;
-  const int w = blockIdx.x + 1, h = blockIdx.y / PARTS, part = blockIdx.y % PARTS, G = pg.Hq / pg.Hkv;
-  const int4 here = pg.cuts[w], prev = pg.cuts[w - 1];
-  if (here.z == 0 || here.x >= pg.r.B) return;
-  if (prev.x == here.x && prev.y == here.y && prev.z > 0) return;      // an earlier workgroup's
-  int pieces = 1;
-  for (int v = w; v < pg.width; v += 64) {                             // this one and those behind it that start in the same block
-    const int mine = v + (threadIdx.x & 63);
-    int4 x = make_int4(-1, 0, 0, 0);
-    if (mine < pg.width) x = pg.cuts[mine];
-    const unsigned long long other = ~__ballot(x.x == here.x && x.y == here.y && x.z > 0);
-    pieces += other ? __builtin_ctzll(other) : 64;
-    if (other) break;
-  }
-  const ChunkExtent e = chunk_extent(pg.r, pg.c, here.x);
-  const int r = part * ROWS + threadIdx.x / (D / 4), d = threadIdx.x % (D / 4) * 4;      // row of the workgroup
-  const int ctx = e.len - e.n, base = PipePlan::first_row(e);
-  const unsigned row = (unsigned)((max(ctx, 0) - base) * G) / 32u * 32u + here.y * kPipeRows + r, at = row / (unsigned)G;      // (PipePlan::first_wave)
-  const int hq = h * G + (int)(row - at * G), pos = base + (int)at, i = pos - ctx;
-  if (pos < max(ctx, 0) || i >= e.n) return;
-  const size_t stride = (size_t)2 * pg.Hkv * kPipeRows * (D + 4);      // from a slot of one workgroup to the next one's
-  const float* first = pg.part + ((size_t)(2 * w) * pg.Hkv + h) * kPipeRows * (D + 4) + (size_t)r * (D + 4);       // slot 2 w; the end before it: 2 w - 1
-  const float* before = first - stride / 2;
-  float m = before[D];
-#pragma unroll 4
-  for (int s = 0; s < pieces - 1; ++s) m = fmaxf(m, first[s * stride + D]);
-  const float f0 = __builtin_amdgcn_exp2f(before[D] - m);
-  float l = before[D + 1] * f0;
-  f32x4 o = *reinterpret_cast<const f32x4*>(before + d) * f0;
-#pragma unroll 4
-  for (int s = 0; s < pieces - 1; ++s) {
-    const float* ps = first + s * stride;
-    const float f = __builtin_amdgcn_exp2f(ps[D] - m);
-    l += ps[D + 1] * f;
-    o += *reinterpret_cast<const f32x4*>(ps + d) * f;
-  }
-  const float inv = 1.f / l;
-  bf16x4 v;
-#pragma unroll
-  for (int k = 0; k < 4; ++k) v[k] = (__bf16)(o[k] * inv);
-  *reinterpret_cast<bf16x4*>(static_cast<uint16_t*>(pg.O) + ((size_t)(e.row0 + i) * pg.Hq + hq) * D + d) = v;
-  if (pg.lse && d == 0) pg.lse[(size_t)hq * pg.r.total + e.row0 + i] = m * 0.6931471805599453f + logf(l);
-}
-
-struct PipeChunkPlan {
-  int width;             // workgroups per KV head
-  size_t smem, cuts, workspace;          // cuts: their offset in the workspace
-};
 
 hipError_t launch_chunk_pipe_d128(const ChunkArgs& a, const PipeChunkPlan& p, hipStream_t s);
 hipError_t launch_chunk_pipe_d64(const ChunkArgs& a, const PipeChunkPlan& p, hipStream_t s);
@@ -77,9 +23,8 @@ hipError_t launch_chunk_pipe(const ChunkArgs& a, const PipeChunkPlan& p, hipStre
   auto kernel = chunk_pipe_kernel<D>;
   const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)p.smem);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)(p.width * a.Hkv)), dim3(64 * kPipeWaves), p.smem, s, a);
-  if (p.width > 1)
-    hipLaunchKernelGGL((chunk_pipe_join_kernel<D>), dim3(p.width - 1, a.Hkv * kPipeRows / (kJoinThreads / (D / 4))), dim3(kJoinThreads), 0, s, a);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(p.width * a.Hkv)), dim3(64 * PipeBf16::WAVES), p.smem, s, a);
+  launch_chunk_join<uint16_t, PipeBf16, D>(a, p, s);
   return hipGetLastError();
 }
 

@@ -163,9 +163,7 @@ void launch_chunk_merge(const ChunkArgs& a, int items, int rows, hipStream_t s) 
 struct RowPlan {
   ChunkPlan p;
   int waves, rows16, rows, items;
-  bool block;            // fp32: chunk_block_f32_kernel
 };
-constexpr int kBlockRows = 128;          // rows of one of its workgroups
 hipError_t launch_chunk_bf16(const ChunkArgs& a, int D, const RowPlan& r, hipStream_t s);
 hipError_t launch_chunk_f32(const ChunkArgs& a, int D, const RowPlan& r, hipStream_t s);
 

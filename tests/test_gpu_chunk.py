@@ -90,6 +90,26 @@ def test_long_chunk_of_many_heads(seka, Hq, Hkv, n, S):
     check(seka, P.Pages("bf16", [n], [S], Hq, Hkv, 64, 16, seed=n), f"whole blocks {Hq}/{Hkv} {n} {S}")
 
 
+@pytest.mark.parametrize("Hq,Hkv,D", [(6, 2, 64), (6, 2, 128), (7, 1, 64), (5, 5, 128), (9, 1, 128), (20, 1, 64), (32, 32, 64)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_groups_of_any_size(seka, Hq, Hkv, D, dtype):
+    """A wave's 32 rows are a few positions and all heads of a group: first new tokens at any place in 32 positions, blocks with few rows."""
+    new = [n for n in (1, 2, 11, 33, 70, 100) if n * Hq // Hkv <= 1000]
+    lens = [n + c for n, c in zip(new, (31, 64, 45, 0, 95, 300))]
+    check(seka, P.Pages(dtype, new, lens, Hq, Hkv, D, 16, seed=Hq + D), f"groups {Hq}/{Hkv} {D} {dtype}")
+    check(seka, P.Pages(dtype, new[-1:], [lens[-1] + 500], Hq, Hkv, D, 32, seed=Hq), f"one request {Hq}/{Hkv} {D} {dtype}")
+
+
+@pytest.mark.parametrize("Hq,Hkv,n,S", [(256, 64, 300, 900), (192, 64, 130, 700)])
+def test_long_chunk_of_many_heads_f32(seka, Hq, Hkv, n, S):
+    check(seka, P.Pages("f32", [n], [S], Hq, Hkv, 64, 16, seed=n), f"whole blocks {Hq}/{Hkv} {n} {S}")
+
+
+def test_blocks_cut_by_many_workgroups_f32(seka):
+    check(seka, P.Pages("f32", [33], [9000], 4, 1, 128, 16, seed=1), "pieces of one block")
+    check(seka, P.Pages("f32", [100, 1, 0, 17, 1], [5000, 3, 700, 1200, 2000], 4, 1, 64, 32, seed=2), "pieces of mixed requests")
+
+
 def test_blocks_cut_by_many_workgroups(seka):
     """One head: every block of rows is cut into many pieces; requests of very different lengths share workgroups."""
     check(seka, P.Pages("bf16", [33], [9000], 4, 1, 128, 16, seed=1), "pieces of one block")
