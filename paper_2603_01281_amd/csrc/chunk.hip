@@ -221,6 +221,8 @@ hipError_t launch_rows(const ChunkArgs& a, const RowPlan& r, hipStream_t s) {
   return hipGetLastError();
 }
 
+constexpr int kOneRange = 1024;          // cached tokens, bf16: no more than these are one range
+
 // Rows per workgroup, ranges and the bounds of both, from what the host knows: B requests, `total` new tokens of which no request
 // has more than max_q, caches of up to S tokens.
 RowPlan row_plan(int B, int S, int Hq, int Hkv, int D, int dtype, int total, int max_q) {
@@ -248,7 +250,7 @@ RowPlan row_plan(int B, int S, int Hq, int Hkv, int D, int dtype, int total, int
   r.p.max_splits = (int)ranges;
   // and no second kernel where a wave has no more than four blocks, eight of four waves (bf16, 37 requests of up to 24 over 526, 32 / 4 heads, D = 64:
   // 27.4 us in ranges, 12.8 in one each; fp32, 777 tokens in one range: 14.5 us, in ranges 9.9)
-  if (bf16 ? S <= 1024 : few && S <= 512) r.p.max_splits = 1;
+  if (bf16 ? S <= kOneRange : few && S <= 512) r.p.max_splits = 1;
   r.p.streams = (long long)(300e6 / (2.0 * 32 * Hkv * D * (bf16 ? 2 : 4)));
   // sum over chunks of ceil(blocks / L) <= T / L + chunks with T / L <= slots, and no more than every chunk in all its ranges
   r.items = (int)std::min(chunks + (1 << r.p.slots_log2), chunks * r.p.max_splits);
@@ -265,12 +267,15 @@ int compute_units() {
   });
 }
 
-// Products of a call's rows with S keys each, in flops, from which on long chunks go to the pipelined kernel.  us, kernel of few rows / pipelined, 32 / 8
-// heads: 4.3e9 n=128 S=2048 27.7 / 34.1, n=512 S=512 25.0 / 28.1; 24 / 8 heads, about 4e9, three of up to 185 over 1077 42.1 / 29.1; 8.6e9 four of up to 64 over 4096 42.5 / 32.8; 1.6e10
-// n=1000 S=1000 52.4 / 37.9; 3.4e10 n=512 S=4096 103 / 53.5.
-constexpr double kPipeLeastFlops = 3.5e9;
-
-constexpr double kBlockLeastFlops = 1e9;
+// Products of a call's rows with S keys each, in flops, from which on long chunks go to the kernel whose waves have rows of their own; bf16, and its caches
+// that the kernel of few rows takes in one range.  us, few rows / pipelined: 2.2e9 three of up to 153 over 7358, 5 / 5 heads, D = 64, 28.3 / 27.5; 3.2e9 three of up
+// to 11 over 27872, 32 / 4, D = 64, 29.6 / 32.5; 4.9e9 four of up to 194 over 1515, 32 / 8, 37.3 / 32.4; 1.5e10 four of up to 491 over 1354, 24 / 8, 56.3 / 39.3;
+// in one range: 4.9e9 three of up to 942 over 996, 8 / 2, 19.4 / 29.7; 6.8e9 63 of up to 73 over 376, 32 / 8, 32.7 / 37.4; 8.1e9 24 of up to 379 over 379, 30.3 / 26.9.
+constexpr double kPipeLeastFlops = 3.5e9, kPipeLeastFlopsShort = 7.5e9;
+// And fp32, at D = 64 and 128.  us, few rows / blocks: D = 64, 7.7e8 n=75 S=5039 8 / 2 heads 24.9 / 47.4, 1.2e9 ten of up to 26 over 1465 43.0 / 35.8, 3e9
+// n=388 S=934 73.6 / 53.4; D = 128, 5.7e9 four of up to 85 over 14804 5 / 5 heads 91.1 / 107, 1.2e10 ten of up to 58 over 9466 147 / 149, 1.6e10 n=422
+// S=2284 196 / 159, 2.3e10 six of up to 65 over 6984 196 / 162.
+constexpr double kBlockLeastFlops64 = 1e9, kBlockLeastFlops128 = 1.2e10;
 
 // Whether a call's chunks go to a kernel whose waves have rows of their own, and how: more rows per KV head than four tiles of 16, and, bf16, a
 // cache whose page numbers fit beside the tiles in LDS (4 bytes for every page of S tokens).
@@ -278,7 +283,7 @@ bool pipe_plan(int S, int Hq, int Hkv, int D, int dtype, int shift, int total, i
   const int G = Hq / Hkv;
   const bool bf16 = dtype == SEKA_BF16;
   if ((long long)std::min(max_q, total) * G <= 64) return false;
-  if (4.0 * D * total * Hq * S <= (bf16 ? kPipeLeastFlops : kBlockLeastFlops)) return false;
+  if (4.0 * D * total * Hq * S <= (bf16 ? (S <= kOneRange ? kPipeLeastFlopsShort : kPipeLeastFlops) : D == 64 ? kBlockLeastFlops64 : kBlockLeastFlops128)) return false;
   out->width = std::max(1, (bf16 ? 1 : 2) * compute_units() / Hkv);      // workgroups to a compute unit
   out->smem = !bf16 ? 0 : attention_bf16_pipe_smem_bytes(D, 0, false, 1, PipeBf16::WAVES) + (((size_t)S >> shift) + 2) * sizeof(int);
   out->cuts = (size_t)2 * out->width * Hkv * (bf16 ? PipeBf16::ROWS : PipeF32::ROWS) * (D + 4) * sizeof(float);      // behind the states, two per workgroup
