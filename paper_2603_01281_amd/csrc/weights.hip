@@ -324,7 +324,8 @@ __global__ __launch_bounds__(kWtBlockThreads, 4) void weights_block_kernel(Weigh
         wt_rows<decltype(masked)::value, T, NF, KT>(q[r16 & AHEAD], kf, ref, last, kbase, c2, sum);
       }
     };
-    if (ctx + r0 / G < kbase + KEYS - 1) turn(std::true_type{});
+    if (kbase >= e.len) {}                               // wave-uniform: no keys of its own
+    else if (ctx + r0 / G < kbase + KEYS - 1) turn(std::true_type{});
     else turn(std::false_type{});
     if (r0 + kWtRows < rows) place(buf ^ 1);             // read by nobody since the barrier before
     __syncthreads();
