@@ -10,10 +10,11 @@
 // Few rows (generation): HBM-bound, every key is read once.  weights_stream_kernel holds the rows and streams the keys as whole rows
 // through a wave-private LDS tile, a block ahead, over ranges that are cut as for the attention itself (paged.h, plan_item).
 // Many rows: bound by the vector unit (an exponential takes it four times as long as a multiplication; 96 cycles per tile of 16 x 16
-// against 64 of the matrix pipe at D = 128).  weights_block_kernel holds 64 keys per wave in registers and passes the rows by, 64 or 128 at a
-// time through LDS for all its waves; two groups of four waves have the same keys and take half of the rows each (one wave per SIMD had
+// against 64 of the matrix pipe at D = 128).  weights_block_kernel holds 32 keys per wave (fp32, D = 128: 16) in registers and passes the rows by, 64 or 128 at a
+// time through LDS for all its waves; two groups of waves have the same keys and take half of the rows each (one wave per SIMD had
 // nothing to hide its latencies behind: a chunk of 1000 over 8192, 32 / 8 heads, 142 us).  weights_share_kernel, where those would leave compute units idle: 64 keys per workgroup,
 // every wave its share of the rows, straight from the caches; the waves' sums are joined in LDS.
+// One token of 24 requests of up to 8192, 32 / 8 heads, D = 128: 35 us, 4.1 TB/s; two chunks of up to 1000 over 8192: 82 us, 0.77 PFLOP/s.
 #include <algorithm>
 #include <type_traits>
 
@@ -27,8 +28,7 @@ constexpr int kWtWaves = 4, kWtThreads = 64 * kWtWaves;
 // tiles of 16 keys that a wave holds (four of fp32 rows of 512 bytes did not fit its registers)
 template <typename T, int D> constexpr int wt_tiles() { return D * sizeof(T) > 256 ? 2 : 4; }
 template <typename T, int D> constexpr int wt_block_rows() { return D * sizeof(T) > 256 ? 64 : 128; }      // rows that pass through LDS at a time
-constexpr int kWtGroups = 2, kWtBlockWaves = 8;     // groups of waves with the same keys, each with its share of those rows; waves of a group
-constexpr int kWtBlockThreads = 64 * kWtGroups * kWtBlockWaves;
+constexpr int kWtGroups = 2;                // groups of waves with the same keys, each with its share of those rows
 template <typename T, int D> constexpr int wt_block_tiles() { return wt_tiles<T, D>() / 2; }      // 128 registers: four waves to a SIMD
 
 template <typename T> struct WtMath;
@@ -233,9 +233,11 @@ __device__ __forceinline__ void wt_keys(const WeightsArgs& a, const ChunkExtent&
   }
 }
 
-template <typename T, int D>
-__global__ __launch_bounds__(kWtBlockThreads, 4) void weights_block_kernel(WeightsArgs a) {
+// NW: waves of a group.
+template <typename T, int D, int NW>
+__global__ __launch_bounds__(64 * kWtGroups * NW, 4) void weights_block_kernel(WeightsArgs a) {
   typedef typename WtMath<T>::frag frag;
+  constexpr int kWtBlockWaves = NW, kWtBlockThreads = 64 * kWtGroups * NW;
   constexpr int RB = D * sizeof(T), NF = RB / 64, KT = wt_block_tiles<T, D>(), KEYS = 16 * KT, kWtRows = wt_block_rows<T, D>();
   constexpr int CPR = RB / 16, NL = (kWtRows * CPR + kWtBlockThreads - 1) / kWtBlockThreads;    // pieces of a row, loads per thread and turn
   constexpr int LD = RB + 16;
@@ -431,9 +433,14 @@ hipError_t launch(WeightsArgs a, hipStream_t s) {
     return hipGetLastError();
   }
   constexpr int KEYS = 16 * wt_tiles<T, D>();
-  constexpr int kBlock = 16 * wt_block_tiles<T, D>() * kWtBlockWaves;
-  const int blocks = (a.c.cap + kBlock - 1) / kBlock;
-  if ((long long)blocks * a.Hkv * a.r.B >= 256) hipLaunchKernelGGL((weights_block_kernel<T, D>), dim3(blocks, a.Hkv, a.r.B), dim3(kWtBlockThreads), 0, s, a);
+  // Groups of eight waves where the rows are many, and their passage through LDS serves more keys; else of four, two workgroups to a compute unit.  us, eight /
+  // four: 4000 rows, 8192 keys, 32 / 8 heads 82 / 91; 1248 rows of ten requests of up to 1919 48.9 / 34.5; 289 rows, ten of up to 10141, 32 / 32 218 / 190.
+  constexpr int kWave = 16 * wt_block_tiles<T, D>();
+  const int waves = rows > 2048 ? 8 : 4, blocks = (a.c.cap + kWave * waves - 1) / (kWave * waves);
+  const dim3 grid(blocks, a.Hkv, a.r.B), block(64 * kWtGroups * waves);
+  const bool many = (long long)blocks * a.Hkv * a.r.B >= 256;
+  if (many && waves == 8) hipLaunchKernelGGL((weights_block_kernel<T, D, 8>), grid, block, 0, s, a);
+  else if (many) hipLaunchKernelGGL((weights_block_kernel<T, D, 4>), grid, block, 0, s, a);
   else hipLaunchKernelGGL((weights_share_kernel<T, D>), dim3((a.c.cap + KEYS - 1) / KEYS, a.Hkv, a.r.B), threads, 0, s, a);
   return hipGetLastError();
 }
