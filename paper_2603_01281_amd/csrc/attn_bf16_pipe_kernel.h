@@ -1455,9 +1455,13 @@ __device__ __forceinline__ void attention_bf16_pipe_body(const AttnArgs& a, cons
 #pragma unroll
     for (int rt = 0; rt < 2; ++rt) lacc[rt][0] = groups_sum(l_run[rt]);
   }
-  bool joined = false;
-  if constexpr (PAGED) joined = !piece.whole;
-  if (joined) {
+  bool joined = false, some = true;        // some: this wave has rows of the request
+  if constexpr (PAGED) {
+    joined = !piece.whole;
+    some = row_of(0).y < S && row_of(WR - 1).y >= first_new;
+  }
+  if (joined && !some) {
+  } else if (joined) {
     // a part of the block's keys: outputs as they are, reference exponent and sum, for the kernel that joins them
     float* part = nullptr;
     if constexpr (PAGED) part = pg.part + (((size_t)pieces.slot(piece) * nHC + hc) * BQ + WR * rb) * (D + 4);
