@@ -11,17 +11,17 @@ template <typename T, class SHAPE, int D>
 __global__ __launch_bounds__(kJoinThreads) void chunk_pipe_join_kernel(ChunkArgs pg) {
   constexpr int ROWS = kJoinThreads / (D / 4), PARTS = SHAPE::ROWS / ROWS;
   const int w = blockIdx.x + 1, h = blockIdx.y / PARTS, part = blockIdx.y % PARTS, G = pg.Hq / pg.Hkv;
+  const int lane = threadIdx.x & 63;
   const int4 here = pg.cuts[w], prev = pg.cuts[w - 1];
+  int4 mine = pg.cuts[min(w + lane, pg.width - 1)];
   if (here.z == 0 || here.x >= pg.r.B) return;
   if (prev.x == here.x && prev.y == here.y && prev.z > 0) return;      // an earlier workgroup's
   int pieces = 1;
-  for (int v = w; v < pg.width; v += 64) {                             // this one and those behind it that start in the same block
-    const int mine = v + (threadIdx.x & 63);
-    int4 x = make_int4(-1, 0, 0, 0);
-    if (mine < pg.width) x = pg.cuts[mine];
-    const unsigned long long other = ~__ballot(x.x == here.x && x.y == here.y && x.z > 0);
+  for (int v = w;; mine = pg.cuts[min(v + lane, pg.width - 1)]) {      // this one and those behind it that start in the same block
+    const unsigned long long other = ~__ballot(v + lane < pg.width && mine.x == here.x && mine.y == here.y && mine.z > 0);
     pieces += other ? __builtin_ctzll(other) : 64;
-    if (other) break;
+    v += 64;
+    if (other || v >= pg.width) break;
   }
   const ChunkExtent e = chunk_extent(pg.r, pg.c, here.x);
   const int r = part * ROWS + threadIdx.x / (D / 4), d = threadIdx.x % (D / 4) * 4;      // row of the workgroup
@@ -32,14 +32,17 @@ __global__ __launch_bounds__(kJoinThreads) void chunk_pipe_join_kernel(ChunkArgs
   const size_t stride = (size_t)2 * pg.Hkv * SHAPE::ROWS * (D + 4);      // from a slot of one workgroup to the next one's
   const float* first = pg.part + ((size_t)(2 * w) * pg.Hkv + h) * SHAPE::ROWS * (D + 4) + (size_t)r * (D + 4);       // slot 2 w; the end before it: 2 w - 1
   const float* before = first - stride / 2;
-  float m = before[D];
+  // (loads of the two states of a block cut once are on their way together)
+  const float mb = before[D], lb = before[D + 1], m1 = first[D], l1 = first[D + 1];
+  const f32x4 ob = *reinterpret_cast<const f32x4*>(before + d), o1 = *reinterpret_cast<const f32x4*>(first + d);
+  float m = fmaxf(mb, m1);
 #pragma unroll 4
-  for (int s = 0; s < pieces - 1; ++s) m = fmaxf(m, first[s * stride + D]);
-  const float f0 = __builtin_amdgcn_exp2f(before[D] - m);
-  float l = before[D + 1] * f0;
-  f32x4 o = *reinterpret_cast<const f32x4*>(before + d) * f0;
+  for (int s = 1; s < pieces - 1; ++s) m = fmaxf(m, first[s * stride + D]);
+  const float f0 = __builtin_amdgcn_exp2f(mb - m), f1 = __builtin_amdgcn_exp2f(m1 - m);
+  float l = lb * f0 + l1 * f1;
+  f32x4 o = ob * f0 + o1 * f1;
 #pragma unroll 4
-  for (int s = 0; s < pieces - 1; ++s) {
+  for (int s = 1; s < pieces - 1; ++s) {
     const float* ps = first + s * stride;
     const float f = __builtin_amdgcn_exp2f(ps[D] - m);
     l += ps[D + 1] * f;
