@@ -8,6 +8,9 @@
 //   S^T (keys x rows)  = K q^T       A = K rows from LDS, B = queries in registers
 //   O^T (D x rows)    += V^T P^T     A = V^T by transposing LDS reads, B = P^T straight from the S^T accumulators
 // Keys and values are fetched as whole rows into registers, a block ahead, and pass through a wave-private LDS tile.
+// HBM-bound at generation: one token of 24 requests of up to 8192, 32 / 8 heads, D = 128, 277 MB in 64 us, 4.4 TB/s (a large copy 5.2); ranges end
+// up to a block apart and a second kernel of 4 us joins them.  Small calls are two launches' latency: 7 us in one range, 10 in several.
+// Many rows take the kernels whose waves have rows of their own (pipe_plan below).
 #include <algorithm>
 
 #include "chunk_pipe.h"
@@ -109,81 +112,82 @@ __global__ __launch_bounds__(64 * NW, 2) void chunk_rows_bf16_kernel(ChunkArgs a
     }
   };
 
+  // NT where all caches of the call outgrow the last-level cache: keys then leave room for what is read again
   auto run = [&](auto nt) __attribute__((always_inline)) {
-  int kb = k0 + wave * BK;
-  if (kb < k1) {
-    win.load(a.c, it.b, kb, k1);
-    fetch(nt, kb);
-  }
-  row_arrived(qf);
-  for (; kb < k1; kb += NW * BK) {
-    // (a wave's LDS operations execute in program order; the fences are for the compiler)
+    int kb = k0 + wave * BK;
+    if (kb < k1) {
+      win.load(a.c, it.b, kb, k1);
+      fetch(nt, kb);
+    }
+    row_arrived(qf);
+    for (; kb < k1; kb += NW * BK) {
+      // (a wave's LDS operations execute in program order; the fences are for the compiler)
 #pragma unroll
-    for (int x = 0; x < NV; ++x) *reinterpret_cast<u32x4*>(tile + (RPI * x + lane / CPR) * LDK + 8 * (lane % CPR)) = kr[x];
-    asm volatile("" ::: "memory");
-    f32x4 sc[2][RT];
+      for (int x = 0; x < NV; ++x) *reinterpret_cast<u32x4*>(tile + (RPI * x + lane / CPR) * LDK + 8 * (lane % CPR)) = kr[x];
+      asm volatile("" ::: "memory");
+      f32x4 sc[2][RT];
 #pragma unroll
-    for (int kt = 0; kt < 2; ++kt)
+      for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt) sc[kt][rt] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int rt = 0; rt < RT; ++rt) sc[kt][rt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks)
+      for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-      for (int kt = 0; kt < 2; ++kt) {
-        const bf16x8 kf = *reinterpret_cast<const bf16x8*>(tile + (16 * kt + l16) * LDK + 32 * ks + 8 * grp);
+        for (int kt = 0; kt < 2; ++kt) {
+          const bf16x8 kf = *reinterpret_cast<const bf16x8*>(tile + (16 * kt + l16) * LDK + 32 * ks + 8 * grp);
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) sc[kt][rt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[rt][ks], sc[kt][rt], 0, 0, 0);
-      }
-    asm volatile("" ::: "memory");
+          for (int rt = 0; rt < RT; ++rt) sc[kt][rt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[rt][ks], sc[kt][rt], 0, 0, 0);
+        }
+      asm volatile("" ::: "memory");
 #pragma unroll
-    for (int x = 0; x < NV; ++x) *reinterpret_cast<u32x4*>(tile + (RPI * x + lane / CPR) * LDV + 8 * (lane % CPR)) = vr[x];
-    asm volatile("" ::: "memory");
-    const int kb_next = kb + NW * BK;
-    if (kb_next < k1) fetch(nt, kb_next);      // on their way during the softmax
+      for (int x = 0; x < NV; ++x) *reinterpret_cast<u32x4*>(tile + (RPI * x + lane / CPR) * LDV + 8 * (lane % CPR)) = vr[x];
+      asm volatile("" ::: "memory");
+      const int kb_next = kb + NW * BK;
+      if (kb_next < k1) fetch(nt, kb_next);      // on their way during the softmax
 
-    bf16x8 pb[RT];
-    const bool masked = kb + BK - 1 > all_see || kb + BK > k1;
+      bf16x8 pb[RT];
+      const bool masked = kb + BK - 1 > all_see || kb + BK > k1;
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      float t[8];
+      for (int rt = 0; rt < RT; ++rt) {
+        float t[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) t[e] = sc[e >> 2][rt][e & 3] * c2;
-      if (masked) {
+        for (int e = 0; e < 8; ++e) t[e] = sc[e >> 2][rt][e & 3] * c2;
+        if (masked) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (kb + 16 * (e >> 2) + 4 * grp + (e & 3) > last[rt]) t[e] = -INFINITY;
+          for (int e = 0; e < 8; ++e)
+            if (kb + 16 * (e >> 2) + 4 * grp + (e & 3) > last[rt]) t[e] = -INFINITY;
+        }
+        float top = t[0];
+#pragma unroll
+        for (int e = 1; e < 8; ++e) top = fmaxf(top, t[e]);
+        top = groups_max(top);
+        const bool raise = top > m[rt] + kRowSlack;
+        if (__any(raise)) {                  // rare behind the first blocks
+          const float f = raise ? __builtin_amdgcn_exp2f(m[rt] - top) : 1.f;
+          if (raise) m[rt] = top;
+          l[rt] *= f;
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) o[dt][rt] *= f;
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float p = __builtin_amdgcn_exp2f(t[e] - m[rt]);
+          l[rt] += p;                        // of the probabilities before their rounding
+          pb[rt][e] = (__bf16)p;
+        }
       }
-      float top = t[0];
 #pragma unroll
-      for (int e = 1; e < 8; ++e) top = fmaxf(top, t[e]);
-      top = groups_max(top);
-      const bool raise = top > m[rt] + kRowSlack;
-      if (__any(raise)) {                  // rare behind the first blocks
-        const float f = raise ? __builtin_amdgcn_exp2f(m[rt] - top) : 1.f;
-        if (raise) m[rt] = top;
-        l[rt] *= f;
+      for (int dt = 0; dt < DT; ++dt) {
+        // lane: d = 16 dt + l16, slot e <-> key 16 (e / 4) + 4 grp + e % 4, as in the score accumulators
+        const uint16_t* p = tile + (4 * grp + (l16 >> 2)) * LDV + 16 * dt + 4 * (l16 & 3);
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((row_lds_s16x4_ptr)(p));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((row_lds_s16x4_ptr)(p + 16 * LDV));
+        const bf16x8 vf = __builtin_shufflevector(__builtin_bit_cast(bf16x4, lo), __builtin_bit_cast(bf16x4, hi), 0, 1, 2, 3, 4, 5, 6, 7);
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) o[dt][rt] *= f;
+        for (int rt = 0; rt < RT; ++rt) o[dt][rt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pb[rt], o[dt][rt], 0, 0, 0);
       }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float p = __builtin_amdgcn_exp2f(t[e] - m[rt]);
-        l[rt] += p;                        // of the probabilities before their rounding
-        pb[rt][e] = (__bf16)p;
-      }
+      asm volatile("" ::: "memory");         // the tile is rewritten behind these reads
     }
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) {
-      // lane: d = 16 dt + l16, slot e <-> key 16 (e / 4) + 4 grp + e % 4, as in the score accumulators
-      const uint16_t* p = tile + (4 * grp + (l16 >> 2)) * LDV + 16 * dt + 4 * (l16 & 3);
-      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((row_lds_s16x4_ptr)(p));
-      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((row_lds_s16x4_ptr)(p + 16 * LDV));
-      const bf16x8 vf = __builtin_shufflevector(__builtin_bit_cast(bf16x4, lo), __builtin_bit_cast(bf16x4, hi), 0, 1, 2, 3, 4, 5, 6, 7);
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt) o[dt][rt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pb[rt], o[dt][rt], 0, 0, 0);
-    }
-    asm volatile("" ::: "memory");         // the tile is rewritten behind these reads
-  }
   };
   if (it.streams) run(std::true_type{});
   else run(std::false_type{});

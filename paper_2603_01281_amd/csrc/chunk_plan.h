@@ -1,4 +1,4 @@
-// How the blocks of query rows of a batch over a cache of pages are dealt to workgroups (attention_chunk_pipe_kernel).
+// How the blocks of query rows of a batch over a cache of pages are dealt to workgroups (chunk_pipe_kernel, chunk_block_f32_kernel).
 //
 // A request's new tokens are its last n of len cached ones.  Row (p - base) G + g is that of position p and head g of a KV head's group of G,
 // with base the multiple of 32 at or before its first new token: 32 positions are G waves of 32 rows, and no wave's rows lie on both sides of
@@ -7,7 +7,7 @@
 // Block k sees the keys up to its last row, base / 32 + (w0 + WAVES (k + 1)) / G half tiles, with w0 the first wave that has new tokens.  A block costs
 // those and OVER half tiles besides (its start and its output); all costs are in units of a G-th of half a tile.
 //
-// The blocks of all requests in a row are one axis of work of length T, which W workgroups per head chunk cut into equal pieces: a
+// The blocks of all requests in a row are one axis of work of length T, which W workgroups per KV head cut into equal pieces: a
 // piece starts and ends anywhere in a block, at a tile, and the states of a block that was cut are joined by a second kernel.  A
 // single long request (the chunk no longer than what precedes it) takes whole blocks in step, so that the workgroups of an XCD read the same tiles
 // at the same time, and only what is left over by them is cut.

@@ -85,69 +85,69 @@ __global__ __launch_bounds__(kMergeThreads) void chunk_merge_kernel(ChunkArgs a)
   if (splits <= 1) return;
   const int rows = min(a.p.R, it.z * G - it.w);
   for (int r = blockIdx.z; r < rows; r += gridDim.z) {            // workgroup-uniform
-  const int row = it.w + r;
-  const int c = threadIdx.x % LANES, j = threadIdx.x / LANES;
-  const size_t stride = (size_t)a.Hkv * a.p.R * (D + 4);
-  const float* src = a.part + ((size_t)blockIdx.x * a.Hkv + h) * a.p.R * (D + 4) + (size_t)r * (D + 4);
-  float mv[NI], lv[NI];
-  f32x4 ov[NI];
-  auto gather = [&](auto count) __attribute__((always_inline)) {
-    constexpr int N = decltype(count)::value;
+    const int row = it.w + r;
+    const int c = threadIdx.x % LANES, j = threadIdx.x / LANES;
+    const size_t stride = (size_t)a.Hkv * a.p.R * (D + 4);
+    const float* src = a.part + ((size_t)blockIdx.x * a.Hkv + h) * a.p.R * (D + 4) + (size_t)r * (D + 4);
+    float mv[NI], lv[NI];
+    f32x4 ov[NI];
+    auto gather = [&](auto count) __attribute__((always_inline)) {
+      constexpr int N = decltype(count)::value;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const float* ps = src + (size_t)min(j + NJ * i, splits - 1) * stride;
-      mv[i] = ps[D];
-      lv[i] = ps[D + 1];
-      ov[i] = *reinterpret_cast<const f32x4*>(ps + 4 * c);
-    }
-    float m = kRowLow, l = 0.f;
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (j + NJ * i < splits) m = fmaxf(m, mv[i]);
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (j + NJ * i < splits) {
-        const float f = __builtin_amdgcn_exp2f(mv[i] - m);
-        l += lv[i] * f;
-        o += ov[i] * f;
+      for (int i = 0; i < N; ++i) {
+        const float* ps = src + (size_t)min(j + NJ * i, splits - 1) * stride;
+        mv[i] = ps[D];
+        lv[i] = ps[D + 1];
+        ov[i] = *reinterpret_cast<const f32x4*>(ps + 4 * c);
       }
-    sm_o[j][c] = o;
-    if (c == 0) {
-      sm_m[j] = m;
-      sm_l[j] = l;
+      float m = kRowLow, l = 0.f;
+      f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (j + NJ * i < splits) m = fmaxf(m, mv[i]);
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (j + NJ * i < splits) {
+          const float f = __builtin_amdgcn_exp2f(mv[i] - m);
+          l += lv[i] * f;
+          o += ov[i] * f;
+        }
+      sm_o[j][c] = o;
+      if (c == 0) {
+        sm_m[j] = m;
+        sm_l[j] = l;
+      }
+    };
+    if (splits <= NJ) gather(std::integral_constant<int, 1>{});
+    else if (splits <= 2 * NJ) gather(std::integral_constant<int, 2>{});
+    else gather(std::integral_constant<int, NI>{});
+    __syncthreads();
+    if (j == 0) {
+      float m = sm_m[0], l = 0.f;
+      f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 1; k < NJ; ++k) m = fmaxf(m, sm_m[k]);
+#pragma unroll
+      for (int k = 0; k < NJ; ++k) {
+        const float f = __builtin_amdgcn_exp2f(sm_m[k] - m);
+        l += sm_l[k] * f;
+        o += sm_o[k][c] * f;
+      }
+      const int i = row / G, hq = h * G + row % G;
+      const bool some = l > 0.f || l != l;
+      const float inv = some ? 1.f / l : 0.f;
+      T* O = static_cast<T*>(a.O) + ((size_t)(it.y + i) * a.Hq + hq) * D + 4 * c;
+      if constexpr (sizeof(T) == 2) {
+        bf16x4 v;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = (__bf16)(o[k] * inv);
+        *reinterpret_cast<bf16x4*>(O) = v;
+      } else {
+        *reinterpret_cast<f32x4*>(O) = o * inv;
+      }
+      if (a.lse && c == 0) a.lse[(size_t)hq * a.r.total + it.y + i] = some ? m * 0.6931471805599453f + logf(l) : -INFINITY;
     }
-  };
-  if (splits <= NJ) gather(std::integral_constant<int, 1>{});
-  else if (splits <= 2 * NJ) gather(std::integral_constant<int, 2>{});
-  else gather(std::integral_constant<int, NI>{});
-  __syncthreads();
-  if (j == 0) {
-  float m = sm_m[0], l = 0.f;
-  f32x4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int k = 1; k < NJ; ++k) m = fmaxf(m, sm_m[k]);
-#pragma unroll
-  for (int k = 0; k < NJ; ++k) {
-    const float f = __builtin_amdgcn_exp2f(sm_m[k] - m);
-    l += sm_l[k] * f;
-    o += sm_o[k][c] * f;
-  }
-  const int i = row / G, hq = h * G + row % G;
-  const bool some = l > 0.f || l != l;
-  const float inv = some ? 1.f / l : 0.f;
-  T* O = static_cast<T*>(a.O) + ((size_t)(it.y + i) * a.Hq + hq) * D + 4 * c;
-  if constexpr (sizeof(T) == 2) {
-    bf16x4 v;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] = (__bf16)(o[k] * inv);
-    *reinterpret_cast<bf16x4*>(O) = v;
-  } else {
-    *reinterpret_cast<f32x4*>(O) = o * inv;
-  }
-  if (a.lse && c == 0) a.lse[(size_t)hq * a.r.total + it.y + i] = some ? m * 0.6931471805599453f + logf(l) : -INFINITY;
-  }
-  __syncthreads();                         // the next row's states
+    __syncthreads();                         // the next row's states
   }
 }
 

@@ -7,6 +7,8 @@
 // 2. evict_move_kernel: rows of K and V (and the weights) to their new places.  A row moves to an earlier place or stays, so within
 //    one pool a workgroup passes the rows in order, reads a block of rows, waits for all its waves and writes it: no source is
 //    overwritten before it was read.  Between two pools the rows are independent and workgroups share them.
+// 16 requests of 16384, 8 heads of 128, cut to 4096: 108 us: 19 for the selection (the histogram's rounds; 8 MB of weights) and 85 for 413 MB
+// of rows of 256 bytes from anywhere, 4.9 TB/s.  One request of 4097: 14.4 us, of them 10.4 the selection's chain of four rounds.
 #include <algorithm>
 
 #include "paged.h"

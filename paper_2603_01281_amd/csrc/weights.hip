@@ -14,7 +14,7 @@
 // time through LDS for all its waves; two groups of waves have the same keys and take half of the rows each (one wave per SIMD had
 // nothing to hide its latencies behind: a chunk of 1000 over 8192, 32 / 8 heads, 142 us).  weights_share_kernel, where those would leave compute units idle: 64 keys per workgroup,
 // every wave its share of the rows, straight from the caches; the waves' sums are joined in LDS.
-// One token of 24 requests of up to 8192, 32 / 8 heads, D = 128: 35 us, 4.1 TB/s; two chunks of up to 1000 over 8192: 82 us, 0.77 PFLOP/s.
+// One token of 24 requests of up to 8192, 32 / 8 heads, D = 128: 35 us, 4.1 TB/s; 1000 over 8192 beside one: 82 us, 0.77 PFLOP/s.
 #include <algorithm>
 #include <type_traits>
 
