@@ -296,7 +296,7 @@ __device__ __forceinline__ void attention_bf16_pipe_body(const AttnArgs& a, cons
   };
   if constexpr (PAGED) {
     slot = nblocks = qb = 0;
-    if (hc == 0 && threadIdx.x == 0) pg.cuts[item] = make_int4(pieces.start.b, pieces.start.k, pieces.start.t, 0);
+    if (hc == 0 && threadIdx.x == 0) pg.cuts[item] = pieces.note();
     pipe_rows_without_keys<uint16_t, D>(pg, item, hc);
     if (!pieces.next(piece)) return;         // workgroup-uniform, before any barrier
     take_piece();

@@ -197,7 +197,7 @@ __global__ __launch_bounds__(256, 2) void chunk_block_f32_kernel(ChunkArgs a) {
   const int h = blockIdx.x % a.Hkv, item = blockIdx.x / a.Hkv, G = a.Hq / a.Hkv, tid = threadIdx.x;
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, g = lane >> 4;
   PipePieces<PipeF32> pieces(a.r, a.c, a.width, G, item);
-  if (h == 0 && tid == 0) a.cuts[item] = make_int4(pieces.start.b, pieces.start.k, pieces.start.t, 0);
+  if (h == 0 && tid == 0) a.cuts[item] = pieces.note();
   pipe_rows_without_keys<float, D>(a, item, h);
 
   const size_t row_floats = (size_t)a.Hkv * D;

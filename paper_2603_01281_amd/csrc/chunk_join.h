@@ -33,16 +33,25 @@ __global__ __launch_bounds__(kJoinThreads) void chunk_pipe_join_kernel(ChunkArgs
   const float* first = pg.part + ((size_t)(2 * w) * pg.Hkv + h) * SHAPE::ROWS * (D + 4) + (size_t)r * (D + 4);       // slot 2 w; the end before it: 2 w - 1
   const float* before = first - stride / 2;
   // (loads of the two states of a block cut once are on their way together)
-  const float mb = before[D], lb = before[D + 1], m1 = first[D], l1 = first[D + 1];
-  const f32x4 ob = *reinterpret_cast<const f32x4*>(before + d), o1 = *reinterpret_cast<const f32x4*>(first + d);
+  const float mb = before[D], lb = before[D + 1];
+  const f32x4 ob = *reinterpret_cast<const f32x4*>(before + d);
+  float m1 = first[D], l1 = first[D + 1];
+  f32x4 o1 = *reinterpret_cast<const f32x4*>(first + d);
+  if (here.w) {                            // a piece of no tile has left nothing there
+    m1 = mb;
+    l1 = 0.f;
+    o1 = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
   float m = fmaxf(mb, m1);
 #pragma unroll 4
-  for (int s = 1; s < pieces - 1; ++s) m = fmaxf(m, first[s * stride + D]);
+  for (int s = 1; s < pieces - 1; ++s)
+    if (!pg.cuts[w + s].w) m = fmaxf(m, first[s * stride + D]);
   const float f0 = __builtin_amdgcn_exp2f(mb - m), f1 = __builtin_amdgcn_exp2f(m1 - m);
   float l = lb * f0 + l1 * f1;
   f32x4 o = ob * f0 + o1 * f1;
 #pragma unroll 4
   for (int s = 1; s < pieces - 1; ++s) {
+    if (pg.cuts[w + s].w) continue;
     const float* ps = first + s * stride;
     const float f = __builtin_amdgcn_exp2f(ps[D] - m);
     l += ps[D + 1] * f;

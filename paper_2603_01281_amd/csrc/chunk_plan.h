@@ -69,6 +69,8 @@ struct PipePlan {
       if (nb >= W && pipe_first_row(e) >= e.n) {
         rounds = nb / W;
         rem = nb - rounds * W;
+        // the whole blocks count in full in cut(), so here too: their sums then rise and fall once from workgroup to workgroup, and the cuts never go back
+        per = (before(e, nb) + W - 1) / W;
       }
     }
   }
@@ -227,6 +229,11 @@ struct PipePieces {
       return true;
     }
     return false;
+  }
+  // a start inside a block that is the next workgroup's too: no tile, and no state
+  __device__ __forceinline__ int4 note() const {
+    const bool none = start.t > 0 && start.b == end.b && start.k == end.k && start.t == end.t;
+    return make_int4(start.b, start.k, start.t, none);
   }
   // where the state of a piece that is not whole lies: each workgroup has at most two of them
   __device__ __forceinline__ int slot(const PipePiece& x) const { return 2 * w + (x.t0 > 0 ? 0 : 1); }

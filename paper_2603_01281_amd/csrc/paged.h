@@ -193,7 +193,7 @@ struct ChunkArgs {
   float* part;            // partial states: [item, Hkv, R, D + 4]: outputs, reference exponent (base 2), sum
   int Hq, Hkv;
   int width;              // long chunks: workgroups per head chunk (chunk_plan.h)
-  int4* cuts;             // and where each of them starts: request, block, tile
+  int4* cuts;             // and where each of them starts: request, block, tile; whether it has no tile there (PipePieces::note)
   float scale;
 };
 

@@ -41,7 +41,8 @@ struct RotUnit {
   bool is_q, is_v;
   int h, i0, i1, n;      // head; first elements; pairs or elements
 
-  // What every thread would work out again for each of its units; u / per_row is the upper half of u times `inverse`: exact, as u per_row < 2^32.
+  // What every thread would work out again for each of its units; u / per_row is the upper half of u times `inverse`, exact below u per_row = 2^32
+  // (0: a division).
   struct Row {
     int nrot, per_row, turned;
     uint32_t inverse;
@@ -49,7 +50,7 @@ struct RotUnit {
       nrot = (a.half + V - 1) / V;
       per_row = nrot + (a.D - 2 * a.half + V - 1) / V;
       turned = ((a.Q ? a.Hq : 0) + (a.K ? a.Hkv : 0)) * per_row;
-      inverse = per_row == 1 ? 0 : 0xffffffffu / (uint32_t)per_row + 1u;
+      inverse = per_row == 1 || (uint32_t)turned > 0xffffffffu / (uint32_t)per_row ? 0 : 0xffffffffu / (uint32_t)per_row + 1u;
     }
   };
 
@@ -64,7 +65,7 @@ struct RotUnit {
       kind = COPY;
       return;
     }
-    const int row = r.inverse ? (int)__umulhi((uint32_t)u, r.inverse) : u, part = u - row * per_row;
+    const int row = r.inverse ? (int)__umulhi((uint32_t)u, r.inverse) : u / per_row, part = u - row * per_row;
     is_q = row < q_rows;
     h = is_q ? row : row - q_rows;
     if (part >= nrot) {

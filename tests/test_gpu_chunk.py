@@ -105,6 +105,13 @@ def test_long_chunk_of_many_heads_f32(seka, Hq, Hkv, n, S):
     check(seka, P.Pages("f32", [n], [S], Hq, Hkv, 64, 16, seed=n), f"whole blocks {Hq}/{Hkv} {n} {S}")
 
 
+@pytest.mark.parametrize("dtype,Hq,Hkv,n,S", [("f32", 768, 48, 81, 185), ("f32", 1024, 64, 69, 180), ("bf16", 256, 16, 296, 772)])
+def test_few_blocks_left_over(seka, dtype, Hq, Hkv, n, S):
+    """A single request whose blocks go to the workgroups whole, but for one or three that all of them share: pieces of no tile at all
+    (the second and third), and a last block that costs half (the first)."""
+    check(seka, P.Pages(dtype, [n], [S], Hq, Hkv, 64, 16, seed=n), f"left over {dtype} {Hq}/{Hkv} {n} {S}")
+
+
 def test_blocks_cut_by_many_workgroups_f32(seka):
     check(seka, P.Pages("f32", [33], [9000], 4, 1, 128, 16, seed=1), "pieces of one block")
     check(seka, P.Pages("f32", [100, 1, 0, 17, 1], [5000, 3, 700, 1200, 2000], 4, 1, 64, 32, seed=2), "pieces of mixed requests")
