@@ -27,7 +27,8 @@ typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 constexpr int kWtWaves = 4, kWtThreads = 64 * kWtWaves;
 // tiles of 16 keys that a wave holds (four of fp32 rows of 512 bytes did not fit its registers)
 template <typename T, int D> constexpr int wt_tiles() { return D * sizeof(T) > 256 ? 2 : 4; }
-template <typename T, int D> constexpr int wt_block_rows() { return D * sizeof(T) > 256 ? 64 : 128; }      // rows that pass through LDS at a time
+// rows that pass through LDS at a time (no more than two 16-byte pieces to a thread, where there are 128 registers)
+template <typename T, int D, int NW> constexpr int wt_block_rows() { return D * sizeof(T) > 256 || (NW == 4 && D * sizeof(T) == 256) ? 64 : 128; }
 constexpr int kWtGroups = 2;                // groups of waves with the same keys, each with its share of those rows
 template <typename T, int D> constexpr int wt_block_tiles() { return wt_tiles<T, D>() / 2; }      // 128 registers: four waves to a SIMD
 
@@ -238,7 +239,7 @@ template <typename T, int D, int NW>
 __global__ __launch_bounds__(64 * kWtGroups * NW, 4) void weights_block_kernel(WeightsArgs a) {
   typedef typename WtMath<T>::frag frag;
   constexpr int kWtBlockWaves = NW, kWtBlockThreads = 64 * kWtGroups * NW;
-  constexpr int RB = D * sizeof(T), NF = RB / 64, KT = wt_block_tiles<T, D>(), KEYS = 16 * KT, kWtRows = wt_block_rows<T, D>();
+  constexpr int RB = D * sizeof(T), NF = RB / 64, KT = wt_block_tiles<T, D>(), KEYS = 16 * KT, kWtRows = wt_block_rows<T, D, NW>();
   constexpr int CPR = RB / 16, NL = (kWtRows * CPR + kWtBlockThreads - 1) / kWtBlockThreads;    // pieces of a row, loads per thread and turn
   constexpr int LD = RB + 16;
   __shared__ __attribute__((aligned(16))) unsigned char rows_lds[2][kWtRows * LD];
@@ -302,33 +303,48 @@ __global__ __launch_bounds__(64 * kWtGroups * NW, 4) void weights_block_kernel(W
   int buf = 0;
   for (int r0 = r_lo; r0 < rows; r0 += kWtRows, buf ^= 1) {
     if (r0 + kWtRows < rows) fetch(r0 + kWtRows);
-    auto turn = [&](auto masked) __attribute__((always_inline)) {
-      constexpr int NT = kWtRows / 16 / kWtGroups;       // this group's tiles of the rows
-      const int rt0 = group * NT;
-      constexpr int AHEAD = sizeof(T) == 2;              // a tile's rows are read while the one before is worked on (fp32: no registers left)
+    // this group's tiles of the rows: every second one, of those that hold any (all 64 or 128 for a request with one token: fp32, 14 requests of up to
+    // 18 new tokens over 13524, 8 / 2 heads, 45 us, without 35)
+    auto turn = [&](auto masked, auto whole) __attribute__((always_inline)) {
+      constexpr int NT = kWtRows / 16 / kWtGroups;
+      constexpr int AHEAD = sizeof(T) == 2 && decltype(whole)::value;      // a tile's rows are read while the one before is worked on (fp32: no registers left)
       frag q[1 + AHEAD][NF];
       auto read = [&](int r16) __attribute__((always_inline)) {
 #pragma unroll
-        for (int f = 0; f < NF; ++f) q[r16 & AHEAD][f] = *reinterpret_cast<const frag*>(rows_lds[buf] + (16 * (rt0 + r16) + l16) * LD + 64 * f + 16 * grp);
+        for (int f = 0; f < NF; ++f) q[r16 & AHEAD][f] = *reinterpret_cast<const frag*>(rows_lds[buf] + (16 * (kWtGroups * r16 + group) + l16) * LD + 64 * f + 16 * grp);
       };
-      if (AHEAD) read(0);
-#pragma unroll
-      for (int r16 = 0; r16 < NT; ++r16) {
-        if (r16 + AHEAD < NT) read(r16 + AHEAD);
-        const f32x4 ref4 = *reinterpret_cast<const f32x4*>(&ref_lds[buf][16 * (rt0 + r16) + 4 * grp]);
+      auto work = [&](int r16) __attribute__((always_inline)) {
+        const int first = 16 * (kWtGroups * r16 + group) + 4 * grp;
+        const f32x4 ref4 = *reinterpret_cast<const f32x4*>(&ref_lds[buf][first]);
         float ref[4];
         int last[4];
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
           ref[x] = ref4[x];
-          last[x] = decltype(masked)::value ? last_lds[buf][16 * (rt0 + r16) + 4 * grp + x] : 0;
+          last[x] = decltype(masked)::value ? last_lds[buf][first + x] : 0;
         }
         wt_rows<decltype(masked)::value, T, NF, KT>(q[r16 & AHEAD], kf, ref, last, kbase, c2, sum);
+      };
+      if constexpr (decltype(whole)::value) {
+        if (AHEAD) read(0);
+#pragma unroll
+        for (int r16 = 0; r16 < NT; ++r16) {
+          if (r16 + AHEAD < NT) read(r16 + AHEAD);
+          work(r16);
+        }
+      } else {
+        const int n = ((rows - r0 + 15) / 16 - group + kWtGroups - 1) / kWtGroups;
+#pragma nounroll
+        for (int r16 = 0; r16 < n; ++r16) {
+          read(r16);
+          work(r16);
+        }
       }
     };
-    if (kbase >= e.len) {}                               // wave-uniform: no keys of its own
-    else if (ctx + r0 / G < kbase + KEYS - 1) turn(std::true_type{});
-    else turn(std::false_type{});
+    const bool masks = ctx + r0 / G < kbase + KEYS - 1;  // (all wave-uniform)
+    if (kbase >= e.len) {}                               // no keys of its own
+    else if (r0 + kWtRows > rows) turn(std::true_type{}, std::false_type{});
+    else masks ? turn(std::true_type{}, std::true_type{}) : turn(std::false_type{}, std::true_type{});
     if (r0 + kWtRows < rows) place(buf ^ 1);             // read by nobody since the barrier before
     __syncthreads();
   }
@@ -434,7 +450,7 @@ hipError_t launch(WeightsArgs a, hipStream_t s) {
   }
   constexpr int KEYS = 16 * wt_tiles<T, D>();
   // Groups of eight waves where the rows are many, and their passage through LDS serves more keys; else of four, two workgroups to a compute unit.  us, eight /
-  // four: 4000 rows, 8192 keys, 32 / 8 heads 82 / 91; 1248 rows of ten requests of up to 1919 48.9 / 34.5; 289 rows, ten of up to 10141, 32 / 32 218 / 190.
+  // four: 4000 rows, 8192 keys, 32 / 8 heads 82 / 91; 1248 rows of ten requests of up to 1919 48.9 / 36.4; 289 rows, ten of up to 10141, 32 / 32 218 / 175.
   constexpr int kWave = 16 * wt_block_tiles<T, D>();
   const int waves = rows > 2048 ? 8 : 4, blocks = (a.c.cap + kWave * waves - 1) / (kWave * waves);
   const dim3 grid(blocks, a.Hkv, a.r.B), block(64 * kWtGroups * waves);
