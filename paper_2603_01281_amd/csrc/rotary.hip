@@ -6,9 +6,10 @@
 //
 // HBM-bound: every row is read and written once.  A workgroup takes one token (grid.y: a share of its heads); one sine and cosine
 // per pair, which all heads of the token share, go through LDS while the first rows are on their way.  A thread owns whole pairs
-// (16 bytes on each side), so input and output may be the same memory.
+// (16 bytes on each side), the same ones of every row that it takes, so input and output may be the same memory, and finds its place in a row once
+// (a unit's place found by division each time, which is as much work as turning it: 4460 tokens into pages, fp32, 49.8 us).
 // 16381 tokens, 32 + 8 heads of 128, half of each turned: 335 MB in 64 us, 5.2 TB/s, what a large copy reaches; 48 tokens: 3.6 us of a call's 6.6.
-// Into pages, fp32, 4460 tokens: 219 MB in 50 us, 4.4 TB/s (one unit per thread and workgroups for all of them: 60); 64 requests at one token: 4.9 us of a call's 7.
+// Into pages, fp32, 4460 tokens: 219 MB in 47.4 us, 4.6 TB/s; 64 requests at one token: 4.9 us of a call's 7.
 #include <algorithm>
 
 #include "paged.h"
@@ -32,80 +33,38 @@ template <> struct RotElem<float> {
 
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 
-// Work of a token in units: V pairs of a row of Q or K, or V elements that are copied (behind the rotated part; V in the paged form).
-template <typename T, bool PAGED>
-struct RotUnit {
-  static constexpr int V = RotElem<T>::V;
-  enum Kind { PAIRS, PAIRS_BY_ELEMENT, COPY, COPY_BY_ELEMENT };
-  Kind kind;
-  bool is_q, is_v;
-  int h, i0, i1, n;      // head; first elements; pairs or elements
-
-  // What every thread would work out again for each of its units; u / per_row is the upper half of u times `inverse`, exact below u per_row = 2^32
-  // (0: a division).
-  struct Row {
-    int nrot, per_row, turned;
-    uint32_t inverse;
-    __device__ __forceinline__ Row(const RotaryArgs& a) {
-      nrot = (a.half + V - 1) / V;
-      per_row = nrot + (a.D - 2 * a.half + V - 1) / V;
-      turned = ((a.Q ? a.Hq : 0) + (a.K ? a.Hkv : 0)) * per_row;
-      inverse = per_row == 1 || (uint32_t)turned > 0xffffffffu / (uint32_t)per_row ? 0 : 0xffffffffu / (uint32_t)per_row + 1u;
-    }
-  };
-
-  __device__ __forceinline__ RotUnit(const RotaryArgs& a, const Row& r, int u) {
-    const int dim = 2 * a.half, nrot = r.nrot, per_row = r.per_row, q_rows = a.Q ? a.Hq : 0;
-    is_v = PAGED && u >= r.turned;
-    if (is_v) {                              // of all heads' values in a row
-      is_q = false;
-      h = 0;
-      i0 = i1 = (u - r.turned) * V;
-      n = V;
-      kind = COPY;
-      return;
-    }
-    const int row = r.inverse ? (int)__umulhi((uint32_t)u, r.inverse) : u / per_row, part = u - row * per_row;
-    is_q = row < q_rows;
-    h = is_q ? row : row - q_rows;
-    if (part >= nrot) {
-      i0 = i1 = dim + (part - nrot) * V;
-      n = min(V, a.D - i0);
-      kind = dim % V == 0 ? COPY : COPY_BY_ELEMENT;
-    } else {
-      const int p0 = part * V;
-      n = min(V, a.half - p0);
-      i0 = a.interleaved ? 2 * p0 : p0;
-      i1 = a.interleaved ? 2 * p0 + V : a.half + p0;
-      kind = n == V && (a.interleaved || a.half % V == 0) ? PAIRS : PAIRS_BY_ELEMENT;
-    }
-  }
-  __device__ __forceinline__ const T* source(const RotaryArgs& a, int t) const {
-    const void* x = is_v ? a.V : is_q ? a.Q : a.K;
-    return static_cast<const T*>(x) + ((size_t)t * (is_q ? a.Hq : a.Hkv) + h) * a.D;
-  }
-};
-
 template <typename T, bool PAGED>
 __global__ __launch_bounds__(kRotThreads) void rotary_kernel(RotaryArgs a) {
   using E = RotElem<T>;
-  using Unit = RotUnit<T, PAGED>;
   constexpr int V = E::V;
+  enum Kind { PAIRS, PAIRS_BY_ELEMENT, COPY, COPY_BY_ELEMENT };
   __shared__ float cs[64], sn[64];
   const int t = blockIdx.x, tid = threadIdx.x;
-  const typename Unit::Row per(a);
-  const int units = per.turned + (PAGED ? a.Hkv * (a.D / V) : 0), stride = gridDim.y * kRotThreads;
 
-  // the first unit's loads are on their way while the token's place and its angles are found
-  int u = blockIdx.y * kRotThreads + tid;
-  Unit x(a, per, min(u, units - 1));
-  u32x4 v0 = {0, 0, 0, 0}, v1 = {0, 0, 0, 0};
-  auto load = [&]() __attribute__((always_inline)) {
-    const T* src = x.source(a, t);
-    if (x.kind == Unit::PAIRS || x.kind == Unit::COPY) v0 = *reinterpret_cast<const u32x4*>(src + x.i0);
-    if (x.kind == Unit::PAIRS) v1 = *reinterpret_cast<const u32x4*>(src + x.i1);
+  // This thread's part of every row that it takes: V pairs, or V elements behind the rotated ones.
+  const int dim = 2 * a.half, nrot = (a.half + V - 1) / V, per_row = nrot + (a.D - dim + V - 1) / V, step = kRotThreads / per_row;
+  const int part = tid % per_row, q_rows = a.Q ? a.Hq : 0, rows = q_rows + (a.K ? a.Hkv : 0);
+  const bool turns = part < nrot;
+  const int p0 = part * V;                   // its first pair
+  const int i0 = !turns ? dim + (part - nrot) * V : a.interleaved ? 2 * p0 : p0, i1 = !turns ? i0 : a.interleaved ? 2 * p0 + V : a.half + p0;
+  const int n = turns ? min(V, a.half - p0) : min(V, a.D - i0);                  // pairs or elements
+  const Kind kind = turns ? (n == V && (a.interleaved || a.half % V == 0) ? PAIRS : PAIRS_BY_ELEMENT) : dim % V == 0 ? COPY : COPY_BY_ELEMENT;
+  int row = tid < step * per_row ? blockIdx.y * step + tid / per_row : rows;     // the next one: + step gridDim.y
+  const int v_pieces = PAGED ? a.Hkv * (a.D / V) : 0;                            // of all heads' values
+  int piece = blockIdx.y * kRotThreads + tid;
+  auto source = [&](int row) __attribute__((always_inline)) -> const T* {
+    return row < q_rows ? static_cast<const T*>(a.Q) + ((size_t)t * a.Hq + row) * a.D : static_cast<const T*>(a.K) + ((size_t)t * a.Hkv + (row - q_rows)) * a.D;
   };
-  if (u < units) load();
+  // the first loads are on their way while the token's place and its angles are found
+  u32x4 v0 = {0, 0, 0, 0}, v1 = {0, 0, 0, 0}, w = {0, 0, 0, 0};
+  auto load = [&]() __attribute__((always_inline)) {
+    const T* src = source(row);
+    if (kind == PAIRS || kind == COPY) v0 = *reinterpret_cast<const u32x4*>(src + i0);
+    if (kind == PAIRS) v1 = *reinterpret_cast<const u32x4*>(src + i1);
+  };
+  auto load_v = [&]() __attribute__((always_inline)) { w = *reinterpret_cast<const u32x4*>(static_cast<const T*>(a.V) + (size_t)t * a.Hkv * a.D + (size_t)piece * V); };
+  if (row < rows) load();
+  if (PAGED && piece < v_pieces) load_v();
 
   // ---- where the token lies ----
   bool cached = false;
@@ -141,58 +100,68 @@ __global__ __launch_bounds__(kRotThreads) void rotary_kernel(RotaryArgs a) {
   __syncthreads();
 
   const size_t cache_row = ((((size_t)page << a.c.shift) + slot) * a.Hkv) * a.D;
-  while (u < units) {
-    const T* src = x.source(a, t);
-    T* dst = x.is_q ? static_cast<T*>(a.Q_out) + ((size_t)t * a.Hq + x.h) * a.D
-             : PAGED ? static_cast<T*>(x.is_v ? a.c.V : a.c.K) + cache_row + (size_t)x.h * a.D
-                     : static_cast<T*>(a.K_out) + ((size_t)t * a.Hkv + x.h) * a.D;
-    const int p0 = a.interleaved ? x.i0 / 2 : x.i0;
-    if (PAGED && !x.is_q && !cached) {
+  auto target = [&](int row) __attribute__((always_inline)) -> T* {
+    if (row < q_rows) return static_cast<T*>(a.Q_out) + ((size_t)t * a.Hq + row) * a.D;
+    return PAGED ? static_cast<T*>(a.c.K) + cache_row + (size_t)(row - q_rows) * a.D : static_cast<T*>(a.K_out) + ((size_t)t * a.Hkv + (row - q_rows)) * a.D;
+  };
+  while (row < rows) {
+    if (sizeof(T) == 2) asm volatile("" ::: "memory");     // sixteen angles in registers would halve the waves: they are read from LDS for each row
+    const T* src = source(row);
+    T* dst = target(row);
+    if (PAGED && row >= q_rows && !cached) {
       // a token that has no place in the cache
-    } else if (x.kind == Unit::PAIRS) {
+    } else if (kind == PAIRS) {
       T p[V], q[V];
+      float c[V], s[V];                      // of its pairs, the same in every row
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        c[k] = cs[p0 + k];
+        s[k] = sn[p0 + k];
+      }
       __builtin_memcpy(p, &v0, 16);
       __builtin_memcpy(q, &v1, 16);
       if (a.interleaved) {
 #pragma unroll
         for (int k = 0; k < V; k += 2) {
-          const int i = p0 + k / 2, j = i + V / 2;
+          const int i = k / 2, j = i + V / 2;
           const float x0 = E::get(p[k]), x1 = E::get(p[k + 1]), y0 = E::get(q[k]), y1 = E::get(q[k + 1]);
-          p[k] = E::put(x0 * cs[i] - x1 * sn[i]);
-          p[k + 1] = E::put(x1 * cs[i] + x0 * sn[i]);
-          q[k] = E::put(y0 * cs[j] - y1 * sn[j]);
-          q[k + 1] = E::put(y1 * cs[j] + y0 * sn[j]);
+          p[k] = E::put(x0 * c[i] - x1 * s[i]);
+          p[k + 1] = E::put(x1 * c[i] + x0 * s[i]);
+          q[k] = E::put(y0 * c[j] - y1 * s[j]);
+          q[k + 1] = E::put(y1 * c[j] + y0 * s[j]);
         }
       } else {
 #pragma unroll
         for (int k = 0; k < V; ++k) {
           const float x0 = E::get(p[k]), y0 = E::get(q[k]);
-          p[k] = E::put(x0 * cs[p0 + k] - y0 * sn[p0 + k]);
-          q[k] = E::put(y0 * cs[p0 + k] + x0 * sn[p0 + k]);
+          p[k] = E::put(x0 * c[k] - y0 * s[k]);
+          q[k] = E::put(y0 * c[k] + x0 * s[k]);
         }
       }
       __builtin_memcpy(&v0, p, 16);
       __builtin_memcpy(&v1, q, 16);
-      *reinterpret_cast<u32x4*>(dst + x.i0) = v0;
-      *reinterpret_cast<u32x4*>(dst + x.i1) = v1;
-    } else if (x.kind == Unit::COPY) {
-      if (src != dst) *reinterpret_cast<u32x4*>(dst + x.i0) = v0;
-    } else if (x.kind == Unit::COPY_BY_ELEMENT) {
+      *reinterpret_cast<u32x4*>(dst + i0) = v0;
+      *reinterpret_cast<u32x4*>(dst + i1) = v1;
+    } else if (kind == COPY) {
+      if (src != dst) *reinterpret_cast<u32x4*>(dst + i0) = v0;
+    } else if (kind == COPY_BY_ELEMENT) {
       if (src != dst)
-        for (int e = 0; e < x.n; ++e) dst[x.i0 + e] = src[x.i0 + e];
+        for (int e = 0; e < n; ++e) dst[i0 + e] = src[i0 + e];
     } else {
-      for (int k = 0; k < x.n; ++k) {
-        const int e0 = a.interleaved ? x.i0 + 2 * k : x.i0 + k, e1 = a.interleaved ? e0 + 1 : x.i1 + k;
+      for (int k = 0; k < n; ++k) {
+        const int e0 = a.interleaved ? i0 + 2 * k : i0 + k, e1 = a.interleaved ? e0 + 1 : i1 + k;
         const float x0 = E::get(src[e0]), y0 = E::get(src[e1]);
         dst[e0] = E::put(x0 * cs[p0 + k] - y0 * sn[p0 + k]);
         dst[e1] = E::put(y0 * cs[p0 + k] + x0 * sn[p0 + k]);
       }
     }
-    u += stride;
-    if (u < units) {
-      x = Unit(a, per, u);
-      load();
-    }
+    row += step * gridDim.y;
+    if (row < rows) load();
+  }
+  while (PAGED && cached && piece < v_pieces) {
+    *reinterpret_cast<u32x4*>(static_cast<T*>(a.c.V) + cache_row + (size_t)piece * V) = w;
+    piece += kRotThreads * gridDim.y;
+    if (piece < v_pieces) load_v();
   }
   if (PAGED && cached && a.c.W && blockIdx.y == 0 && tid < a.Hkv)
     a.c.W[((size_t)page * a.Hkv + tid) * (1 << a.c.shift) + slot] = a.mask && a.mask[t] ? INFINITY : 0.f;
@@ -202,9 +171,9 @@ __global__ __launch_bounds__(kRotThreads) void rotary_kernel(RotaryArgs a) {
 
 hipError_t launch_rotary(const RotaryArgs& a, int dtype, hipStream_t s) {
   // a workgroup per token, and where those are few so many that every thread has one unit: the rest is waiting for memory
-  const int row_units = (a.D + 15) / 16 * (dtype == SEKA_BF16 ? 1 : 2) + 1;
-  const int units = ((a.Q ? a.Hq : 0) + 2 * (a.K ? a.Hkv : 0)) * row_units;
-  const int most = std::max(1, (units + kRotThreads - 1) / kRotThreads);
+  const int V = dtype == SEKA_BF16 ? 8 : 4, per_row = (a.half + V - 1) / V + (a.D - 2 * a.half + V - 1) / V, step = kRotThreads / per_row;
+  const int rows = (a.Q ? a.Hq : 0) + (a.K ? a.Hkv : 0);
+  const int most = std::max(1, (rows + step - 1) / step);
   const dim3 grid(a.total, std::min(most, std::max(1, 1024 / a.total))), block(kRotThreads);
   if (a.r.B > 0) {
     if (dtype == SEKA_BF16) hipLaunchKernelGGL((rotary_kernel<uint16_t, true>), grid, block, 0, s, a);
