@@ -3,7 +3,7 @@
 //
 // 1. evict_select_kernel, one workgroup per (request, KV head): the weights become ordered integers in LDS; the (budget - recent)-th
 //    largest is found by four rounds of 256 counters over its bytes; waves then write down the places of what stays, each
-//    over its own part of the tokens, with ranks from ballots.
+//    over its own part of the tokens, with ranks from ballots.  Up to kSelFew candidates count the others that come before them instead.
 // 2. evict_move_kernel: rows of K and V (and the weights) to their new places.  A row moves to an earlier place or stays, so within
 //    one pool a workgroup passes the rows in order, reads a block of rows, waits for all its waves and writes it: no source is
 //    overwritten before it was read.  Between two pools the rows are independent and workgroups share them.
@@ -20,6 +20,7 @@ typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64;
 constexpr int kSelCopies = 16;                  // of every counter: lanes that count the same byte meet in one of them
 constexpr int kSelKeys = 30 * 1024;             // tokens whose keys LDS holds
+constexpr int kSelFew = 256;                    // candidates that are ranked by counting (3 requests of up to 207, a call: 9.0 us, in rounds 11.5)
 constexpr int kMoveThreads = 256, kMoveRows = 4;     // rows of a thread whose pieces are in flight together
 
 // Larger weights have larger keys; both zeros the same one; what is not a number the smallest.
@@ -70,6 +71,30 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(EvictArgs a) 
       for (int u = 0; u < U; ++u)
         if (q0 + u * kSelThreads < quads) keys4[q0 + u * kSelThreads] = keys_of(w[u]);
     }
+  }
+  if (m <= kSelFew) {                           // four threads to a candidate, a quarter of the others each
+    __syncthreads();
+    if (tid < 4 * quads - m) keys[m + tid] = 0;                // what is behind the candidates comes before none of them
+    __syncthreads();
+    const int j = tid >> 2;
+    const uint32_t mine = j < m ? keys[j] : 0xffffffffu;
+    int before = 0;                             // keys that come before its own
+#pragma unroll 4
+    for (int q = tid & 3; q < quads; q += 4) {
+      const u32x4 u = keys4[q];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) before += (int)(u[x] > mine) + (int)((u[x] == mine) & (4 * q + x < j));
+    }
+    before += __shfl_xor(before, 1);
+    before += __shfl_xor(before, 2);
+    const bool stays = j < m && before < want;
+    const unsigned long long all = __ballot(stays && (tid & 3) == 0);
+    if (lane == 0) sm_gt[wave] = __popcll(all);
+    __syncthreads();
+    int at = __popcll(all & ((1ull << lane) - 1));
+    for (int w = 0; w < wave; ++w) at += sm_gt[w];
+    if (stays && (tid & 3) == 0) kept[at] = j;
+    return;
   }
   for (int k = tid; k < 256 * kSelCopies; k += kSelThreads) hist[0][k] = 0;
   __syncthreads();

@@ -87,6 +87,22 @@ def test_weights_of_all_kinds(seka, kind):
     check(seka, x, 123, 11, f"weights: {kind}")
 
 
+@pytest.mark.parametrize("kind", ["any", "equal", "few values", "infinities and nan"])
+@pytest.mark.parametrize("budget,recent", [(12, 11), (30, 11), (200, 11), (9, 0)])
+def test_few_candidates(seka, kind, budget, recent):
+    x = P.Pages("f32", [0] * 7, [40, 13, 266, 267, 268, 75, 331], 2, 2, 64, 16, seed=8)
+    g = np.random.default_rng(9)
+    if kind == "equal":
+        x.W[:] = 0.25
+    elif kind == "few values":
+        x.W[:] = g.integers(0, 3, x.W.shape)
+    elif kind != "any":
+        x.W[g.random(x.W.shape) < 0.3] = np.inf
+        x.W[g.random(x.W.shape) < 0.3] = -np.inf
+        x.W[g.random(x.W.shape) < 0.3] = np.nan
+    check(seka, x, budget, recent, f"few candidates: {kind} {budget} {recent}")
+
+
 def test_more_tokens_than_shared_memory_holds(seka):
     x = P.Pages("bf16", [0], [40001], 1, 1, 64, 64, seed=4)
     x.W[:] = np.round(x.W * 500) / 500                     # many ties
