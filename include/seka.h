@@ -310,7 +310,7 @@ seka_status seka_head_distance(const void* h_pos, const void* h_neg, const seka_
  * cu_seqlens[b] .. cu_seqlens[b+1]-1, the first max_q of them; they are the LAST n tokens of its cache, so new token i is
  * cached token lens[b] - n + i (lens counts the tokens with the new ones, before and after the chunk's keys are written).
  * Every length, offset and page number is clamped on the device, so no content of cu_seqlens, lens or table can make a
- * kernel leave the tensors; rows that belong to no request are left untouched.
+ * kernel leave the tensors; rows that belong to no request are left untouched.  A call has fewer than 2^24 new tokens.
  */
 typedef struct {
   void* K;                /* dev [num_pages, page_size, Hkv, D] tensor dtype                        */
@@ -354,7 +354,7 @@ seka_status seka_rope_frequencies(int32_t dim, double base, int32_t scaling, dou
  *   out = factor * (x cos - y sin, y cos + x sin) for each pair (x, y), angles formed in 64 bits, one rounding to the dtype
  *
  * Q, Q_out  dev [B,S,Hq,D];  K, K_out dev [B,S,Hkv,D] or both NULL;  tensor dtype.  Q_out == Q and K_out == K are allowed,
- *           any other overlap is SEKA_ERR_ALIAS.  (A packed batch is B = 1, S = total_tokens, with positions.)
+ *           any other overlap is SEKA_ERR_ALIAS.  (A packed batch is B = 1, S = total_tokens, with positions.)  B*S < 2^24.
  * positions dev [B*S] int32, any values, or NULL: token t of every row of the batch has position t.
  * The inverse rotation is the one of -freq.
  */

@@ -117,6 +117,8 @@ size_t pool_bytes(const seka_paged* c, const seka_shape* sh) {
 }
 size_t pool_weight_bytes(const seka_paged* c, const seka_shape* sh) { return (size_t)c->num_pages * c->page_size * sh->Hkv * sizeof(float); }
 
+constexpr int64_t kMaxNewTokens = 1 << 24;       // a workgroup of 256 threads each, in a grid of fewer than 2^32 threads
+
 seka_status check_paged(const seka_paged* c, const seka_shape* sh, bool need_w, bool need_lens) {
   if (!c || !c->K || !c->V || !c->table || (need_lens && !c->lens) || (need_w && !c->W)) return SEKA_ERR_NULL;
   if (c->num_pages < 1 || c->max_pages < 1) return SEKA_ERR_SHAPE;
@@ -142,7 +144,7 @@ seka::PagedCache paged(const seka_paged* c, const seka_shape* sh) {
 seka_status check_chunk(const int32_t* cu, int64_t total, int32_t max_q, const seka_shape* sh, seka::ChunkRows* r) {
   if (!cu) return SEKA_ERR_NULL;
   if (reinterpret_cast<uintptr_t>(cu) & 3u) return SEKA_ERR_ALIGN;
-  if (total < 1 || total > 0x7fffffffLL || max_q < 1 || max_q > sh->S) return SEKA_ERR_SHAPE;
+  if (total < 1 || total >= kMaxNewTokens || max_q < 1 || max_q > sh->S) return SEKA_ERR_SHAPE;
   r->cu = cu; r->B = sh->B; r->total = (int)total; r->max_q = max_q;
   return SEKA_OK;
 }
@@ -485,7 +487,7 @@ seka_status seka_rotary(const void* Q, void* Q_out, const void* K, void* K_out, 
   seka::RotaryArgs a = {};
   if ((rc = check_rope(rope, sh, &a)) != SEKA_OK) return rc;
   const int64_t total = (int64_t)sh->B * sh->S;
-  if (total > 0x7fffffffLL) return SEKA_ERR_SHAPE;
+  if (total >= kMaxNewTokens) return SEKA_ERR_SHAPE;
   if (misaligned(Q) || misaligned(Q_out) || misaligned(K) || misaligned(K_out) || (reinterpret_cast<uintptr_t>(positions) & 3u)) return SEKA_ERR_ALIGN;
   const size_t nq = (size_t)total * sh->Hq * sh->D * elem_size(sh->dtype), nk = K ? (size_t)total * sh->Hkv * sh->D * elem_size(sh->dtype) : 0;
   if ((Q_out != Q && ranges_overlap(Q_out, nq, Q, nq)) ||
@@ -536,7 +538,7 @@ seka_status seka_cache_append(const void* K, const void* V, const void* Q, void*
 }
 
 size_t seka_chunk_workspace_bytes(const seka_shape* sh, int64_t total_tokens, int32_t max_q) {
-  if (check_shape(sh, true) != SEKA_OK || sh->B > kMaxGridYZ || total_tokens < 1 || total_tokens > 0x7fffffffLL || max_q < 1 || max_q > sh->S) return 0;
+  if (check_shape(sh, true) != SEKA_OK || sh->B > kMaxGridYZ || total_tokens < 1 || total_tokens >= kMaxNewTokens || max_q < 1 || max_q > sh->S) return 0;
   return seka::chunk_workspace_bytes(sh->B, sh->S, sh->Hq, sh->Hkv, sh->D, sh->dtype, (int)total_tokens, max_q);
 }
 

@@ -108,6 +108,15 @@ def test_chunk_refuses(B):
     assert B.seka_chunk_workspace_bytes(2, 4096, 4, 2, 64, B.SEKA_BF16, 10, 4097) == 0 and B.seka_chunk_workspace_bytes(2, 4096, 4, 2, 65, B.SEKA_BF16, 10, 5) == 0
 
 
+def test_more_new_tokens_than_a_grid_holds(B):
+    s, one, n = shape(B), shape(B, Hq=1, Hkv=1, B=1 << 12, S=1 << 12), 1 << 24
+    assert B.lib.seka_rotary(AT(5), AT(6), None, None, ref(one), ref(rope(B)), None, None) == SHAPE
+    assert B.lib.seka_cache_append(AT(5), AT(6), None, None, ref(s), ref(paged(B)), None, None, None, AT(11), n, 5, None) == SHAPE
+    assert B.lib.seka_attention_chunk(AT(5), AT(6), None, ref(s), ref(paged(B)), AT(8), n, 5, AT(9), 64 * MB, None) == SHAPE
+    assert B.lib.seka_attention_weights(AT(5), AT(6), ref(s), ref(paged(B)), None, AT(8), n, 5, 5, ctypes.c_float(1.0), None) == SHAPE
+    assert B.seka_chunk_workspace_bytes(2, 128, 4, 2, 64, B.SEKA_BF16, n, 5) == 0
+
+
 def test_weights_refuse(B):
     def call(Q=AT(5), lse=AT(6), sh=None, c=None, W_in=AT(7), cu=AT(8), total=10, max_q=5, window=5, decay=1.0):
         return B.lib.seka_attention_weights(Q, lse, ref(sh or shape(B)), ref(c or paged(B)), W_in, cu, total, max_q, window, decay, None)
